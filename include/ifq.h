@@ -667,6 +667,207 @@ IFQ_API ifq_status ifq_run_stack_static(const ifq_stack* s, const void* x, void*
 /* Bytes of the static workspace of ifq_run_stack_static. Host. */
 IFQ_API size_t ifq_static_workspace_bytes(void);
 
+/* -------------------------------------------------------------------------
+ * Operators for serving language models. What +-1 weights and codes of one
+ * step per layer cannot carry is held in low-bit codes with finer scales: the
+ * products of the layers that the conversion leaves out in 8-bit floats with
+ * a scale for each block of 128, keys and values of past tokens in 4-bit
+ * codes with an offset and a step for each row.
+ *
+ * Rows are dense in their last axis; strides and leading dimensions count
+ * elements. All entry points below that take a stream are asynchronous on it,
+ * allocate nothing and can be captured. Errors are the same throughout:
+ * INVALID_ARGUMENT (a value out of its domain, a missing or misaligned
+ * pointer), UNSUPPORTED (a size or alignment no kernel takes),
+ * INSUFFICIENT_BUFFER (workspace), HIP.
+ * ------------------------------------------------------------------------- */
+
+#define IFQ_TYPE_BF16 0
+#define IFQ_TYPE_F16 1
+#define IFQ_TYPE_F32 2
+
+/*
+ * Quantizer to 8-bit floats (e4m3: 4 exponent and 3 mantissa bits, largest
+ * value 448, no infinities) with one scale per block of block_rows x 128.
+ *   rows, k      the matrix; both may be 0 (nothing is done)
+ *   ld_x         elements from row to row of x, >= k
+ *   ld_codes     bytes from row to row of codes, >= k, a multiple of 16
+ *   x_type       IFQ_TYPE_BF16, F16 or F32
+ *   block_rows   1 (activations: a scale per row) or 128 (weights)
+ */
+typedef struct ifq_f8_quant_desc {
+  int64_t rows, k;
+  int64_t ld_x, ld_codes;
+  int32_t x_type, block_rows;
+} ifq_f8_quant_desc;
+
+/*
+ * codes = e4m3(x * 448 / t), scale = t / 448 with t the block's largest |x|,
+ * at least 2^-96; in fp32: both divisions correctly rounded, ties of the
+ * codes to even. A block that holds a NaN or an infinity gets the scale NaN
+ * and codes 0, so that every product with it is NaN.
+ *   x        device [rows][ld_x], aligned to its element
+ *   codes    device [rows][ld_codes] bytes, 16-byte aligned; columns from k up
+ *            to the next multiple of 16 become 0
+ *   scales   device float [ceil(k/128)][ceil(rows/block_rows)]
+ */
+IFQ_API ifq_status ifq_f8_quantize(const ifq_f8_quant_desc* d, const void* x, void* codes,
+                                   float* scales, hipStream_t stream);
+
+/*
+ * Product of 8-bit float matrices with a scale per block of 128:
+ *   y[i][j] = sum over b of a_scales[b][i] * w_scales[b][j/128]
+ *             * (sum over k in block b of a[i][k] * w[j][k])
+ * with sums in fp32, rounded once to y's type.
+ *   m, n, k      k a multiple of 16 (a shorter row is filled up with zeros, as
+ *                ifq_f8_quantize leaves it); m or n may be 0
+ *   ld_a, ld_w   bytes from row to row, >= k, multiples of 16
+ *   ld_y         elements from row to row of y, >= n
+ *   y_type       IFQ_TYPE_BF16, F16 or F32
+ */
+typedef struct ifq_f8_matmul_desc {
+  int64_t m, n, k;
+  int64_t ld_a, ld_w, ld_y;
+  int32_t y_type, reserved;
+} ifq_f8_matmul_desc;
+
+/*
+ * Device workspace bytes of ifq_f8_matmul for d (may be 0): where few tiles
+ * would leave most of the GPU idle, k is split over workgroups and the parts
+ * are added in a fixed order by the one that ends last. Same rules as
+ * ifq_conv_workspace_bytes: zero-filled before its first use, left ready by
+ * every call, one stream at a time. Host.
+ */
+IFQ_API size_t ifq_f8_matmul_workspace_bytes(const ifq_f8_matmul_desc* d);
+
+/*
+ *   a, w               device e4m3 codes [m][ld_a] and [n][ld_w], 16-byte aligned
+ *   a_scales           device float [ceil(k/128)][m] (ifq_f8_quantize, block_rows 1)
+ *   w_scales           device float [ceil(k/128)][ceil(n/128)] (block_rows 128)
+ *   y                  device [m][ld_y], aligned to its element
+ *   ws                 workspace of ws_bytes >= ifq_f8_matmul_workspace_bytes(d)
+ */
+IFQ_API ifq_status ifq_f8_matmul(const ifq_f8_matmul_desc* d, const void* a,
+                                 const float* a_scales, const void* w, const float* w_scales,
+                                 void* y, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * A paged cache of keys and values in 4-bit codes, and a batch of sequences
+ * in it. A row x (one token's key or value of one head) is held as
+ *   offset o = min(x) rounded down to bfloat16,
+ *   step   t = ((max(x) - o) / 15) rounded up to bfloat16,
+ *   codes  c = rint((x - o) / t) in 0..15        (fp32; t = 0: codes 0)
+ * and stands for o + t*c. A row with a NaN or an infinity, or whose spread
+ * overflows fp32, stands for NaN throughout.
+ *
+ * The cache is num_pages pages of kv_heads * page_tokens * (head_dim + 8)
+ * bytes. A page holds for each head: the keys' codes, the values' codes, and
+ * a word (o in its low half, t in its high half) for each key, then for each
+ * value. Key codes: [token][head_dim/2], 8 dims in 4 bytes, dim 2p+h (of 8) in
+ * nibble p+4h. Value codes, in blocks of 32 tokens: [head_dim/64][16g+n][b]
+ * words of 8 tokens of the dim 64*block+16b+n, token 16u+4g+r (of 32) in
+ * nibble p+4h with 4u+r = 2p+h. These are the orders in which matrix
+ * instructions take their operands, so attention loads 16 bytes per lane and
+ * permutes nothing.
+ *
+ *   batch        sequences
+ *   total_q      rows of new tokens (queries), over all sequences
+ *   max_q        the most new tokens of one sequence
+ *   max_kv       about how long the longest sequence is; only the split of
+ *                the work goes by it, any value >= 0 gives the same result
+ *   heads, kv_heads, head_dim
+ *                query heads (a multiple of kv_heads), key/value heads, and
+ *                values per head: 64, 128 or 256
+ *   page_tokens  tokens per page: a multiple of 32 up to 4096
+ *   num_pages, max_pages
+ *                pages of the cache, and per sequence in the page table
+ *   type         of q, k, v and what is computed from them: IFQ_TYPE_BF16 or F16
+ *   causal       attention: 1: the query at position p sees positions <= p,
+ *                0: all of its sequence (window must be 0)
+ *   window, sinks
+ *                attention: with window > 0, only the last window positions up
+ *                to p, and the first sinks of the sequence
+ *   rot_dim, rot_adjacent, rot_len
+ *                append: the first rot_dim dims (a multiple of 16, 0: none) are
+ *                rotated in pairs, (i, i + rot_dim/2) or with rot_adjacent
+ *                (2i, 2i+1); the tables hold rot_len positions
+ *   scale        attention: factor of the scores
+ *   q_stride, k_stride, v_stride, o_stride
+ *                elements from token to token of q, k, v and the attention's
+ *                output (multiples of 8); heads follow one another
+ *
+ * Device arrays of the batch, the same for all three calls:
+ *   offsets  int32 [batch+1]: sequence b's new tokens are rows offsets[b] ..
+ *            offsets[b+1]-1 (at most max_q)
+ *   lengths  int32 [batch]: its tokens in the cache with the new ones, so that
+ *            new token i is at position lengths[b] - count + i
+ *   pages    int32 [batch][max_pages]: where its positions page_tokens*s .. are
+ * A position outside the page table, or on a page outside 0..num_pages-1, is
+ * not stored, reads as 0 and is not visible. Two sequences must not append to
+ * the same 32 tokens of a page in one call.
+ */
+typedef struct ifq_kv_desc {
+  int32_t batch, total_q, max_q, max_kv;
+  int32_t heads, kv_heads, head_dim, page_tokens;
+  int32_t num_pages, max_pages, type, causal;
+  int32_t window, sinks, rot_dim, rot_adjacent;
+  int32_t rot_len;
+  float scale;
+  int64_t q_stride, k_stride, v_stride, o_stride;
+} ifq_kv_desc;
+
+/* Bytes of the cache of d (0 if d is invalid). Host. */
+IFQ_API size_t ifq_kv_cache_bytes(const ifq_kv_desc* d);
+
+/*
+ * Append the new tokens: rotate each key in fp32 by its position, code it and
+ * its value and store both; other tokens keep their codes. The queries are
+ * rotated on the way.
+ *   q        device [total_q][q_stride], nullable; k, v likewise with their
+ *            strides; 16-byte aligned
+ *   cosines, sines
+ *            device float [rot_len][rot_dim/2], 16-byte aligned (NULL iff
+ *            rot_dim is 0). A position from rot_len on is not stored, and its
+ *            query is passed on as it is.
+ *   q_out    device [total_q][heads][head_dim] dense, NULL iff q is
+ */
+IFQ_API ifq_status ifq_kv_append(const ifq_kv_desc* d, const void* q, const void* k,
+                                 const void* v, const float* cosines, const float* sines,
+                                 const int32_t* offsets, const int32_t* lengths,
+                                 const int32_t* pages, void* cache, void* q_out,
+                                 hipStream_t stream);
+
+/*
+ * Read the rows of the new tokens back, as the values they stand for rounded
+ * to d's type: k_out, v_out device [total_q][kv_heads][head_dim] dense,
+ * 16-byte aligned. With offsets and lengths of any other span it reads that span.
+ */
+IFQ_API ifq_status ifq_kv_read(const ifq_kv_desc* d, const int32_t* offsets,
+                               const int32_t* lengths, const int32_t* pages, const void* cache,
+                               void* k_out, void* v_out, hipStream_t stream);
+
+/*
+ * Device workspace bytes of ifq_kv_attention for d (may be 0): sequences are
+ * split over workgroups where there are few, and the parts joined in a fixed
+ * order by the one that ends last. Rules as for ifq_conv_workspace_bytes. Host.
+ */
+IFQ_API size_t ifq_kv_attention_workspace_bytes(const ifq_kv_desc* d);
+
+/*
+ * Attention of the new tokens over their sequences' cached rows:
+ *   out[i] = sum over visible j of softmax_j(scale * q[i].k[j]) v[j]
+ * with k, v the values that the rows stand for, scores and sums in fp32. Query
+ * head h reads key/value head h / (heads / kv_heads). A query that sees
+ * nothing gives 0.
+ *   q      device [total_q][q_stride], 16-byte aligned
+ *   out    device [total_q][o_stride], 16-byte aligned
+ *   ws     workspace of ws_bytes >= ifq_kv_attention_workspace_bytes(d)
+ */
+IFQ_API ifq_status ifq_kv_attention(const ifq_kv_desc* d, const void* q, const int32_t* offsets,
+                                    const int32_t* lengths, const int32_t* pages,
+                                    const void* cache, void* out, void* ws, size_t ws_bytes,
+                                    hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

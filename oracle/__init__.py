@@ -13,6 +13,8 @@ the GPU library:
                  (O_float), used as the invariant the integer path must meet
   brute.py       pure-Python loops for tiny layers
   layout.py      the 2-bit packed code layout (4 codes per byte along C)
+  serve.py       the operators for serving language models: 8-bit float codes
+                 and their product, the cache of 4-bit codes, attention
 
 Parity status per function (what pins it is in the tests):
   conv acc       pinned: brute force, float64 conv2d of integer tensors,

@@ -43,8 +43,13 @@ IFQ_LAYER_CONV_POOL_FP4 = 4
 
 IFQ_MAX_THRESHOLDS = 15
 
+IFQ_TYPE_BF16 = 0
+IFQ_TYPE_F16 = 1
+IFQ_TYPE_F32 = 2
+
 i32 = ctypes.c_int32
 i64 = ctypes.c_int64
+f32 = ctypes.c_float
 f64 = ctypes.c_double
 vp = ctypes.c_void_p
 dp = ctypes.POINTER(ctypes.c_double)
@@ -94,6 +99,25 @@ class Layer(ctypes.Structure):
 class Stack(ctypes.Structure):
     _fields_ = [("n_layers", i32), ("n_slots", i32),
                 ("layers", ctypes.POINTER(Layer)), ("events", vp)]
+
+
+class F8QuantDesc(ctypes.Structure):
+    _fields_ = [("rows", i64), ("k", i64), ("ld_x", i64), ("ld_codes", i64),
+                ("x_type", i32), ("block_rows", i32)]
+
+
+class F8MatmulDesc(ctypes.Structure):
+    _fields_ = [("m", i64), ("n", i64), ("k", i64), ("ld_a", i64), ("ld_w", i64),
+                ("ld_y", i64), ("y_type", i32), ("reserved", i32)]
+
+
+class KvDesc(ctypes.Structure):
+    _fields_ = [("batch", i32), ("total_q", i32), ("max_q", i32), ("max_kv", i32),
+                ("heads", i32), ("kv_heads", i32), ("head_dim", i32), ("page_tokens", i32),
+                ("num_pages", i32), ("max_pages", i32), ("type", i32), ("causal", i32),
+                ("window", i32), ("sinks", i32), ("rot_dim", i32), ("rot_adjacent", i32),
+                ("rot_len", i32), ("scale", f32), ("q_stride", i64), ("k_stride", i64),
+                ("v_stride", i64), ("o_stride", i64)]
 
 
 def address(t):
@@ -170,13 +194,22 @@ SIGNATURES = [
     ("ifq_run_stack", i32, [ctypes.POINTER(Stack), vp, vp, vp, size_t, vp]),
     ("ifq_run_stack_static", i32, [ctypes.POINTER(Stack), vp, vp, vp]),
     ("ifq_static_workspace_bytes", size_t, []),
+    ("ifq_f8_quantize", i32, [ctypes.POINTER(F8QuantDesc), vp, vp, vp, vp]),
+    ("ifq_f8_matmul_workspace_bytes", size_t, [ctypes.POINTER(F8MatmulDesc)]),
+    ("ifq_f8_matmul", i32, [ctypes.POINTER(F8MatmulDesc), vp, vp, vp, vp, vp, vp, size_t, vp]),
+    ("ifq_kv_cache_bytes", size_t, [ctypes.POINTER(KvDesc)]),
+    ("ifq_kv_append", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+    ("ifq_kv_read", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp]),
+    ("ifq_kv_attention_workspace_bytes", size_t, [ctypes.POINTER(KvDesc)]),
+    ("ifq_kv_attention", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp, size_t, vp]),
 ]
 
 # the launching entry points that api.py calls through _ifqcall, in the order
 # its bind() takes their addresses
 CALLED = ["ifq_conv_forward", "ifq_conv_forward_fp4", "ifq_conv_pool_forward",
           "ifq_conv_pool_forward_fp4", "ifq_maxpool_codes", "ifq_convert_codes",
-          "ifq_run_stack", "ifq_run_stack_static"]
+          "ifq_run_stack", "ifq_run_stack_static", "ifq_f8_quantize", "ifq_f8_matmul",
+          "ifq_kv_append", "ifq_kv_read", "ifq_kv_attention"]
 
 _lib = None
 call = None     # the _ifqcall module, bound to the library

@@ -12,6 +12,7 @@ import numpy as np
 
 from . import _ffi
 from ._ffi import (ConvDesc, FoldParams, JoinParams, Join, PoolDesc, Stack,
+                   F8QuantDesc, F8MatmulDesc, KvDesc,
                    IFQ_OK, IFQ_JOIN_NONE, IFQ_MAX_THRESHOLDS)
 
 
@@ -372,3 +373,97 @@ def ifq_conv_forward_variant(desc, x, w_packed, thr, y, variant, join=None, acc_
         ctypes.byref(desc), _ptr(x), _ptr(w_packed), _ptr(thr),
         ctypes.byref(join) if join is not None else None, _ptr(y), _ptr(acc_dump),
         int(variant), _stream(stream)), "ifq_conv_forward_variant")
+
+
+# -- operators for serving language models ---------------------------------------
+def f8_quant_desc(rows, k, x_type, block_rows=1, ld_x=None, ld_codes=None):
+    """ld_codes None: k up to the next multiple of 16."""
+    return F8QuantDesc(rows, k, k if ld_x is None else ld_x,
+                       -(-k // 16) * 16 if ld_codes is None else ld_codes, x_type, block_rows)
+
+
+def f8_matmul_desc(m, n, k, y_type, ld_a=None, ld_w=None, ld_y=None):
+    return F8MatmulDesc(m, n, k, k if ld_a is None else ld_a, k if ld_w is None else ld_w,
+                        n if ld_y is None else ld_y, y_type, 0)
+
+
+def kv_desc(batch, total_q, max_q, max_kv, heads, kv_heads, head_dim, page_tokens, num_pages,
+            max_pages, type, scale=1.0, causal=True, window=0, sinks=0, rot_dim=0,
+            rot_adjacent=False, rot_len=0, q_stride=None, k_stride=None, v_stride=None,
+            o_stride=None):
+    """Strides None: dense rows of all heads."""
+    qrow, krow = heads * head_dim, kv_heads * head_dim
+    return KvDesc(batch, total_q, max_q, max_kv, heads, kv_heads, head_dim, page_tokens,
+                  num_pages, max_pages, type, int(causal), window, sinks, rot_dim,
+                  int(rot_adjacent), rot_len, scale, qrow if q_stride is None else q_stride,
+                  krow if k_stride is None else k_stride,
+                  krow if v_stride is None else v_stride, qrow if o_stride is None else o_stride)
+
+
+def ifq_f8_quantize(desc, x, codes, scales, stream=None):
+    rc = _ffi.call.f8_quantize(_struct(desc, F8QuantDesc), x, codes, scales, _stream(stream))
+    if rc:
+        _check(rc, "ifq_f8_quantize")
+
+
+def ifq_f8_matmul_workspace_bytes(desc):
+    return int(_lib().ifq_f8_matmul_workspace_bytes(ctypes.byref(desc)))
+
+
+def ifq_f8_matmul(desc, a, a_scales, w, w_scales, y, ws=None, stream=None):
+    """ws None: a zero-filled device workspace is made for this call where it
+    needs one, as for ifq_conv_forward."""
+    d, st = _struct(desc, F8MatmulDesc), _stream(stream)
+    rc = _ffi.call.f8_matmul(d, a, a_scales, w, w_scales, y, ws, _nbytes(ws), st)
+    if rc == _ffi.IFQ_ERR_INSUFFICIENT_BUFFER and ws is None:
+        ws = _workspace(ifq_f8_matmul_workspace_bytes(desc), y, st)
+        rc = _ffi.call.f8_matmul(d, a, a_scales, w, w_scales, y, ws, _nbytes(ws), st)
+    if rc:
+        _check(rc, "ifq_f8_matmul")
+
+
+def _workspace(nbytes, like, stream):
+    """A zero-filled workspace on like's device for one call on that stream
+    (a handle): made, filled and given back in the stream's order."""
+    import torch
+    with torch.cuda.device(like.device):
+        if stream == _stream(None):
+            return torch.zeros(nbytes, dtype=torch.uint8, device=like.device)
+        on = torch.cuda.ExternalStream(stream)
+        with torch.cuda.stream(on):
+            return torch.zeros(nbytes, dtype=torch.uint8, device=like.device)
+
+
+def ifq_kv_cache_bytes(desc):
+    return int(_lib().ifq_kv_cache_bytes(ctypes.byref(desc)))
+
+
+def ifq_kv_append(desc, q, k, v, cosines, sines, offsets, lengths, pages, cache, q_out,
+                  stream=None):
+    rc = _ffi.call.kv_append(_struct(desc, KvDesc), q, k, v, cosines, sines, offsets, lengths,
+                             pages, cache, q_out, _stream(stream))
+    if rc:
+        _check(rc, "ifq_kv_append")
+
+
+def ifq_kv_read(desc, offsets, lengths, pages, cache, k_out, v_out, stream=None):
+    rc = _ffi.call.kv_read(_struct(desc, KvDesc), offsets, lengths, pages, cache, k_out, v_out,
+                           _stream(stream))
+    if rc:
+        _check(rc, "ifq_kv_read")
+
+
+def ifq_kv_attention_workspace_bytes(desc):
+    return int(_lib().ifq_kv_attention_workspace_bytes(ctypes.byref(desc)))
+
+
+def ifq_kv_attention(desc, q, offsets, lengths, pages, cache, out, ws=None, stream=None):
+    """ws None: as for ifq_f8_matmul."""
+    d, st = _struct(desc, KvDesc), _stream(stream)
+    rc = _ffi.call.kv_attention(d, q, offsets, lengths, pages, cache, out, ws, _nbytes(ws), st)
+    if rc == _ffi.IFQ_ERR_INSUFFICIENT_BUFFER and ws is None:
+        ws = _workspace(ifq_kv_attention_workspace_bytes(desc), out, st)
+        rc = _ffi.call.kv_attention(d, q, offsets, lengths, pages, cache, out, ws, _nbytes(ws),
+                                    st)
+    if rc:
+        _check(rc, "ifq_kv_attention")

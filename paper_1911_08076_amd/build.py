@@ -22,7 +22,8 @@ ARCH = "gfx950"
 
 SOURCES = ["ifq_api.cpp", "ifq_conv.hip", "ifq_conv_mfma.hip", "ifq_conv_halo.hip", "ifq_conv_w2.hip", "ifq_conv_wp.hip", "ifq_conv_win.hip",
            "ifq_noalloc.hip",
-           "ifq_conv_small.hip", "ifq_pool.hip", "ifq_thresholds.hip"]
+           "ifq_conv_small.hip", "ifq_pool.hip", "ifq_thresholds.hip",
+           "ifq_serve.cpp", "ifq_f8.hip", "ifq_kv.hip", "ifq_attn.hip"]
 
 
 def build(verbose=False):

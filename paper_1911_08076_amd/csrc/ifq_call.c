@@ -25,6 +25,11 @@ static struct {
   __typeof__(&ifq_convert_codes) convert_codes;
   __typeof__(&ifq_run_stack) run_stack;
   __typeof__(&ifq_run_stack_static) run_stack_static;
+  __typeof__(&ifq_f8_quantize) f8_quantize;
+  __typeof__(&ifq_f8_matmul) f8_matmul;
+  __typeof__(&ifq_kv_append) kv_append;
+  __typeof__(&ifq_kv_read) kv_read;
+  __typeof__(&ifq_kv_attention) kv_attention;
 } fn;
 static PyObject* s_data_ptr;   /* "data_ptr" */
 static PyObject* conv_ptr;     /* the binding's conversion of other tensor arguments */
@@ -107,13 +112,21 @@ ENTRY(convert_codes, "iiiiiittp",
                     P(8)))
 ENTRY(run_stack, "ptttip", run_stack(P(0), P(1), P(2), P(3), (size_t)v[4], P(5)))
 ENTRY(run_stack_static, "pttp", run_stack_static(P(0), P(1), P(2), P(3)))
+ENTRY(f8_quantize, "ptttp", f8_quantize(P(0), P(1), P(2), P(3), P(4)))
+ENTRY(f8_matmul, "pttttttip",
+      f8_matmul(P(0), P(1), P(2), P(3), P(4), P(5), P(6), (size_t)v[7], P(8)))
+ENTRY(kv_append, "pttttttttttp",
+      kv_append(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), P(11)))
+ENTRY(kv_read, "pttttttp", kv_read(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7)))
+ENTRY(kv_attention, "pttttttt" "ip",
+      kv_attention(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), (size_t)v[8], P(9)))
 
 /* bind(address, integer, addresses in the order of the table above) */
 static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t na) {
-  int64_t v[8];
+  int64_t v[13];
   (void)self;
-  if (na != 10) return PyErr_Format(PyExc_TypeError, "bind: 10 arguments expected");
-  if (values(args + 2, 8, "pppppppp", v)) return NULL;
+  if (na != 15) return PyErr_Format(PyExc_TypeError, "bind: 15 arguments expected");
+  if (values(args + 2, 13, "ppppppppppppp", v)) return NULL;
   Py_INCREF(args[0]);
   Py_XSETREF(conv_ptr, args[0]);
   Py_INCREF(args[1]);
@@ -126,6 +139,11 @@ static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t na) {
   fn.convert_codes = P(5);
   fn.run_stack = P(6);
   fn.run_stack_static = P(7);
+  fn.f8_quantize = P(8);
+  fn.f8_matmul = P(9);
+  fn.kv_append = P(10);
+  fn.kv_read = P(11);
+  fn.kv_attention = P(12);
   Py_RETURN_NONE;
 }
 
@@ -133,7 +151,9 @@ static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t na) {
 static PyMethodDef methods[] = {M(bind), M(conv_forward), M(conv_forward_fp4),
                                 M(conv_pool_forward), M(conv_pool_forward_fp4),
                                 M(maxpool_codes), M(convert_codes), M(run_stack),
-                                M(run_stack_static), {NULL, NULL, 0, NULL}};
+                                M(run_stack_static), M(f8_quantize), M(f8_matmul),
+                                M(kv_append), M(kv_read), M(kv_attention),
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ifqcall", NULL, -1, methods,
                                     NULL, NULL, NULL, NULL};
 

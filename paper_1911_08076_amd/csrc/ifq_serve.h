@@ -1,0 +1,69 @@
+// Internals of the operators for serving language models: the 8-bit float
+// quantizer and block-scaled product (ifq_f8.hip), the paged cache of 4-bit
+// codes (ifq_kv.hip) and attention over it (ifq_attn.hip). Arguments reach the
+// launchers validated (ifq_serve.cpp).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "ifq.h"
+#include "ifq_internal.h"
+
+namespace ifq {
+
+constexpr int kF8Block = 128;    // values under one scale of an 8-bit float row
+constexpr int kCodeTokens = 32;  // tokens of one block of value codes in a page
+constexpr int64_t kMaxGroups = (1 << 24) - 1;   // workgroups of 256 of one launch: 2^32 threads
+
+struct KvArgs {
+  const int32_t* offsets;        // [batch + 1] rows of the new tokens
+  const int32_t* lengths;        // [batch] cached tokens, the new ones included
+  const int32_t* pages;          // [batch][max_pages]
+  uint8_t* cache;
+  int64_t page_bytes, head_bytes;
+  int32_t batch, total_q, max_q, heads, kv_heads, page_tokens, num_pages, max_pages;
+};
+
+hipError_t launch_f8_quantize(const ifq_f8_quant_desc& d, const void* x, void* codes,
+                              float* scales, hipStream_t stream);
+
+size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d);
+hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a, const float* a_scales,
+                            const void* w, const float* w_scales, void* y, void* ws,
+                            hipStream_t stream);
+
+hipError_t launch_kv_append(const ifq_kv_desc& d, const void* q, const void* k, const void* v,
+                            const float* cosines, const float* sines, const KvArgs& a,
+                            void* q_out, hipStream_t stream);
+hipError_t launch_kv_read(const ifq_kv_desc& d, const KvArgs& a, void* k_out, void* v_out,
+                          hipStream_t stream);
+
+size_t kv_attention_workspace_bytes(const ifq_kv_desc& d);
+hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs& a, void* out,
+                               void* ws, hipStream_t stream);
+
+#ifdef __HIPCC__
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bits_f32(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ uint32_t f32_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+
+// Offset and step of a cached row, two bfloat16 in a word.
+__device__ __forceinline__ float row_offset(uint32_t w) { return bits_f32(w << 16); }
+__device__ __forceinline__ float row_step(uint32_t w) { return bits_f32(w & 0xFFFF0000u); }
+
+// x / d correctly rounded, given inv = 1 / d correctly rounded: the product
+// is within an ulp, and its remainder, exact in the fma, corrects it.
+__device__ __forceinline__ float div_by(float x, float d, float inv) {
+  const float q = x * inv;
+  return __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
+}
+#endif
+
+}  // namespace ifq

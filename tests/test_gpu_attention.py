@@ -1,0 +1,261 @@
+"""Attention over the paged cache of 4-bit codes on the GPU, against the
+oracle's softmax in 64 bits over the values that the rows stand for. The
+oracle gives the bound on the error before the output is rounded (its
+docstring); the rounding adds half a unit in the last place."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1911_08076_amd as P
+from oracle import serve as S
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": (torch.bfloat16, P.IFQ_TYPE_BF16, 2.0 ** -8, 0.0),
+         "f16": (torch.float16, P.IFQ_TYPE_F16, 2.0 ** -11, 2.0 ** -25)}
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x, np.int32), device=DEV)
+
+
+class Case:
+    def __init__(self, rng, new, lens, heads, kv_heads, dim, page, kind="bf16", causal=True,
+                 window=0, sinks=0, spread=1.0, max_kv=None, pad=0, q_mean=0.0):
+        self.new, self.lens, self.heads, self.kv_heads = new, lens, heads, kv_heads
+        self.dim, self.page, self.kind = dim, page, kind
+        self.causal, self.window, self.sinks = causal, window, sinks
+        self.scale = spread / dim ** 0.5
+        most = max(1, -(-max(max(lens), 1) // page))
+        pages = len(new) * most + 2
+        self.table = rng.permutation(pages)[:len(new) * most].reshape(len(new), most)
+        # what no sequence holds is anything: NaN and infinity among it
+        self.cache = rng.integers(0, 256, (pages, kv_heads, page * (dim + 8)), dtype=np.uint8)
+        self.cache.reshape(-1)[::7] = 255
+        self.rows = []
+        for b, n in enumerate(lens):
+            heads_of = []
+            for g in range(kv_heads):
+                x = rng.standard_normal((2, n, dim)) * np.exp(0.5 * rng.standard_normal((2, 1, dim)))
+                x[1] += 0.5
+                kw, kc = S.row_codes(x[0])
+                vw, vc = S.row_codes(x[1])
+                heads_of.append((kw, kc, vw, vc))
+                for i, id in enumerate(self.table[b][:-(-n // page)]):
+                    self._fill(id, g, i * page, kw, kc, vw, vc)
+            self.rows.append(heads_of)
+        self.offs = np.concatenate([[0], np.cumsum(new)])
+        total = int(self.offs[-1])
+        self.stride = heads * dim + pad
+        dtype, code = TYPES[kind][:2]
+        self.q = torch.from_numpy(rng.standard_normal((max(total, 1), self.stride)) * 1.5 +
+                                  q_mean).to(dtype)
+        self.desc = P.kv_desc(len(new), total, max(new), max(lens) if max_kv is None else max_kv,
+                              heads, kv_heads, dim, page, pages, most, code, scale=self.scale,
+                              causal=causal, window=window, sinks=sinks, q_stride=self.stride,
+                              o_stride=self.stride)
+
+    def _fill(self, id, g, first, kw, kc, vw, vc):
+        """The format's places, a page at a time."""
+        head = S.head_of(self.cache, id, g, self.page, self.dim)
+        n = min(self.page, len(kw) - first)
+        t, d = np.arange(n)[:, None], np.arange(self.dim)[None]
+        head.kw[:n], head.vw[:n] = kw[first:first + n], vw[first:first + n]
+        nib = d % 8 // 2 + 4 * (d % 2)
+        c = kc[first:first + n]
+        for h in (0, 1):
+            at = np.nonzero(nib[0] % 2 == h)[0]
+            byte = at // 8 * 4 + nib[0, at] // 2
+            head.k[:n][:, byte] = (head.k[:n][:, byte] & (0xF0 if h == 0 else 0x0F)) | (
+                c[:, at] << (4 * h))
+        at, sh = S.Page._v_place(t, d)
+        sh = np.broadcast_to(sh, (n, self.dim)).astype(np.uint32)
+        at = [np.broadcast_to(a, (n, self.dim)) for a in at]
+        for one in range(8):
+            i = np.nonzero(sh == 4 * one)
+            place = tuple(a[i] for a in at)
+            head.v[place] = (head.v[place] & ~np.uint32(15 << (4 * one)) & np.uint32(0xFFFFFFFF)) | (
+                vc[first:first + n][i].astype(np.uint32) << np.uint32(4 * one))
+
+    def expected(self):
+        total = int(self.offs[-1])
+        out, bound = np.zeros((2, total, self.heads, self.dim))
+        q = self.q.float().numpy()[:, :self.heads * self.dim].reshape(-1, self.heads, self.dim)
+        for b, n in enumerate(self.new):
+            pos = self.lens[b] - n + np.arange(n)
+            if not self.causal:
+                pos = np.full(n, self.lens[b] - 1)
+            at = slice(self.offs[b], self.offs[b + 1])
+            for h in range(self.heads):
+                rows = self.rows[b][h * self.kv_heads // self.heads]
+                out[at, h], bound[at, h] = S.attention(q[at, h], *rows, pos, self.scale,
+                                                       self.window, self.sinks)
+        return out, bound
+
+    def run(self, ws=None, stream=None, cache=None, table=None):
+        total = int(self.offs[-1])
+        out = torch.full((max(total, 1), self.stride), 55.0, dtype=self.q.dtype, device=DEV)
+        cache = torch.from_numpy(self.cache).to(DEV) if cache is None else cache
+        P.ifq_kv_attention(self.desc, self.q.to(DEV), i32(self.offs), i32(self.lens),
+                           i32(self.table if table is None else table), cache, out, ws=ws,
+                           stream=stream)
+        torch.cuda.synchronize()
+        return out
+
+    def check(self, **kw):
+        out = self.run(**kw).double().cpu().numpy()
+        used = self.heads * self.dim
+        assert (out[:, used:] == 55).all()
+        total = int(self.offs[-1])
+        got = out[:total, :used].reshape(total, self.heads, self.dim)
+        want, bound = self.expected()
+        u, least = TYPES[self.kind][2:]
+        bound = bound + u * (np.abs(want) + bound) + least
+        worst = (np.abs(got - want) / np.maximum(bound, 1e-300)).max() if total else 0.0
+        assert worst <= 1 or (got == want).all(), worst
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,page", [
+    ([1], [1], 1, 1, 32), ([1], [2], 4, 1, 32), ([1, 1], [31, 33], 8, 2, 32),
+    ([1, 1, 1], [32, 64, 129], 16, 2, 64), ([1], [700], 40, 2, 96), ([1], [257], 17, 1, 64)])
+def test_one_token(kind, dim, new, lens, heads, kv_heads, page, rng):
+    Case(rng, new, lens, heads, kv_heads, dim, page, kind).check()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,lens,heads,kv_heads", [
+    ([2, 3], [2, 40], 4, 2), ([17], [17], 2, 2), ([5, 33, 1], [70, 33, 100], 8, 2),
+    ([70], [150], 5, 1), ([130, 64], [130, 200], 4, 1), ([300], [310], 2, 1)])
+def test_many_tokens(kind, dim, new, lens, heads, kv_heads, rng):
+    Case(rng, new, lens, heads, kv_heads, dim, 64, kind).check()
+
+
+@pytest.mark.parametrize("new,lens", [([1, 1], [500, 40]), ([40, 3], [300, 50]), ([200], [260])])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (7, 1), (32, 4), (100, 33), (1000, 4), (64, 64)])
+def test_window_and_sinks(new, lens, window, sinks, rng):
+    Case(rng, new, lens, 4, 2, 64, 32, "f16", window=window, sinks=sinks).check()
+
+
+@pytest.mark.parametrize("new,lens", [([1, 0, 1], [0, 5, 3]), ([8, 4], [3, 0]),
+                                      ([40, 100], [20, 33])])
+def test_queries_that_see_nothing(new, lens, rng):
+    """Sequences shorter than what asks, and empty ones."""
+    Case(rng, new, lens, 4, 2, 128, 32).check()
+    Case(rng, new, lens, 4, 2, 64, 32, "f16", window=6, sinks=2).check()
+
+
+@pytest.mark.parametrize("new,lens", [([1], [90]), ([20, 3], [70, 200]), ([150], [180])])
+def test_not_causal(new, lens, rng):
+    Case(rng, new, lens, 6, 2, 64, 32, causal=False).check()
+
+
+@pytest.mark.parametrize("max_kv", [0, 100, 3000, 10 ** 6])
+def test_long_sequences_split(max_kv, rng):
+    """The hint of the longest length changes the split, not the result."""
+    Case(rng, [1, 1], [2900, 1500], 8, 2, 64, 64, "f16", max_kv=max_kv).check()
+    Case(rng, [2, 1], [1033, 3000], 4, 1, 128, 64, "bf16", max_kv=max_kv, spread=6.0).check()
+
+
+def test_sharp_and_flat_scores(rng):
+    Case(rng, [1, 9], [600, 300], 8, 2, 128, 32, "f16", spread=20.0).check()
+    Case(rng, [1, 9], [600, 300], 8, 2, 128, 32, "f16", spread=0.0).check()
+    Case(rng, [1, 9], [600, 300], 8, 2, 128, 32, "bf16", spread=-3.0).check()
+    Case(rng, [1, 9], [600, 300], 8, 2, 128, 32, "f16", q_mean=2.0).check()
+
+
+def test_rows_with_strides(rng):
+    Case(rng, [1, 1], [100, 50], 4, 2, 64, 32, pad=24).check()
+    Case(rng, [90, 1], [100, 50], 4, 2, 128, 32, pad=8).check()
+
+
+def test_visible_nan_reaches_only_those_that_see_it(rng):
+    c = Case(rng, [4, 60], [40, 80], 4, 2, 64, 32)
+    for b, p in ((0, 38), (1, 50)):
+        head = S.head_of(c.cache, c.table[b, p // 32], 1, 32, 64)
+        head.vw[p % 32] = 0x7FC0
+    out = c.run().double().cpu().numpy().reshape(64, 4, 64)
+    bad = np.isnan(out)
+    want = np.zeros((64, 4, 64), bool)
+    want[2:4, 2:] = True               # queries at 38, 39 of the first sequence
+    want[4 + 30:, 2:] = True           # queries at 50 .. 79 of the second
+    assert np.array_equal(bad, want)
+
+
+def test_pages_the_cache_does_not_have(rng):
+    """Their tokens are not visible."""
+    for new in ([1], [30]):
+        c = Case(rng, new, [100], 4, 2, 64, 32)
+        c.table[0, 1], c.table[0, 2] = -1, len(c.cache)
+        c.rows[0] = [tuple(np.delete(a, np.s_[32:96], 0) for a in r) for r in c.rows[0]]
+        got = c.run().double().cpu().numpy().reshape(-1, 4, 64)
+        c.lens = [36]
+        if new == [30]:                # queries at 70 .. 95 see the first page alone
+            c.new, c.offs = [4], np.array([0, 4])
+            assert np.isfinite(got[:26]).all()
+            got, c.q = got[26:], c.q[26:]
+        want, bound = c.expected()
+        assert (np.abs(got - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
+
+
+def test_same_bits_with_and_without_workspace_and_on_a_stream(rng):
+    c = Case(rng, [1, 1, 1], [5000, 700, 64], 8, 2, 128, 64)
+    n = P.ifq_kv_attention_workspace_bytes(c.desc)
+    ws = torch.zeros(max(n, 1), dtype=torch.uint8, device=DEV)
+    outs = [c.run(), c.run(ws=ws), c.run(ws=ws), c.run(stream=torch.cuda.Stream())]
+    assert all(torch.equal(outs[0], o) for o in outs[1:])
+    assert not ws[:65536].any()
+
+
+def test_pages_past_4_gib(rng):
+    c = Case(rng, [1, 20], [300, 90], 4, 2, 128, 64)
+    size = c.cache[0].size
+    pages = (5 << 30) // size
+    big = torch.zeros(pages, 2, c.cache.shape[2], dtype=torch.uint8, device=DEV)
+    first = pages - len(c.cache)
+    big[first:] = torch.from_numpy(c.cache).to(DEV)
+    c.desc.num_pages = pages
+    c.check(cache=big, table=c.table + first)
+
+
+def test_replayed_graph(rng):
+    """Append and attention in a graph, replayed between other work: lengths and
+    values change on the device, the graph does not."""
+    c = Case(rng, [1, 1], [130, 2000], 8, 2, 128, 64)
+    lens, offs, table = i32(c.lens), i32(c.offs), i32(c.table)
+    cache = torch.from_numpy(c.cache).to(DEV)
+    new = torch.zeros(2, 12, 128, dtype=torch.bfloat16, device=DEV)
+    d = c.desc
+    d.k_stride = d.v_stride = d.q_stride = 12 * 128
+    att = P.kv_desc(2, 2, 1, 2000, 8, 2, 128, 64, d.num_pages, d.max_pages, d.type,
+                    scale=c.scale)
+    q = torch.empty(2, 8, 128, dtype=torch.bfloat16, device=DEV)
+    out = torch.empty_like(q)
+    n = P.ifq_kv_attention_workspace_bytes(att)
+    ws = torch.zeros(max(n, 1), dtype=torch.uint8, device=DEV)
+
+    def step(cache, out):
+        P.ifq_kv_append(d, new, new[:, 8:], new[:, 10:], None, None, offs, lens, table, cache, q)
+        P.ifq_kv_attention(att, q, offs, lens, table, cache, out, ws=ws if n else None)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(cache, out)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cache, out)
+    for i in range(4):
+        new.normal_()
+        lens.sub_(i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager, there = torch.empty_like(out), cache.clone()
+        step(there, eager)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, out) and torch.equal(there, cache)
+        assert out.isfinite().all() and out.abs().sum() > 0

@@ -1,0 +1,201 @@
+"""The quantizer to 8-bit floats and the block-scaled product on the GPU.
+
+Codes and scales are defined step by step in fp32 and must be equal bit for
+bit. A product in fp32 of terms a*w*s, added in any order within and over the
+blocks of 128, is off by at most (128 + blocks + 4) * 2^-23 of the sum of the
+terms' magnitudes (2^-23: each addition may truncate), before it is rounded to
+the output's type."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1911_08076_amd as P
+from oracle import serve as S
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": (torch.bfloat16, P.IFQ_TYPE_BF16, 2.0 ** -8),
+         "f16": (torch.float16, P.IFQ_TYPE_F16, 2.0 ** -11),
+         "f32": (torch.float32, P.IFQ_TYPE_F32, 2.0 ** -24)}
+
+
+def quantize(x, block_rows=1, ld_codes=None, k=None):
+    """x: 2-D device tensor (its stride counts) -> codes, scales on the host."""
+    rows = x.shape[0]
+    k = x.shape[1] if k is None else k
+    kind = {v[0]: v[1] for v in TYPES.values()}[x.dtype]
+    d = P.f8_quant_desc(rows, k, kind, block_rows, ld_x=x.stride(0) if rows > 1 else k,
+                        ld_codes=ld_codes)
+    codes = torch.full((rows, d.ld_codes), 0xAB, dtype=torch.uint8, device=DEV)
+    scales = torch.full((-(-k // 128), -(-rows // block_rows)), -7.0, device=DEV)
+    P.ifq_f8_quantize(d, x, codes, scales)
+    return codes.cpu().numpy(), scales.cpu().numpy()
+
+
+def check_quantize(x, block_rows=1, ld_codes=None):
+    k = x.shape[1]
+    got, gs = quantize(x, block_rows, ld_codes)
+    want, ws = S.f8_quantize(x.float().cpu().numpy(), block_rows)
+    assert np.array_equal(gs, ws, equal_nan=True)
+    assert np.array_equal(got[:, :k], want)
+    k16 = -(-k // 16) * 16
+    assert not got[:, k:k16].any() and (got[:, k16:] == 0xAB).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,k,block_rows", [
+    (1, 1, 1), (1, 128, 1), (1, 4096, 1), (3, 129, 1), (15, 2050, 1), (16, 512, 1),
+    (17, 520, 1), (130, 1000, 1), (1, 7, 128), (128, 128, 128), (129, 300, 128), (300, 64, 128)])
+def test_quantize(kind, rows, k, block_rows, rng):
+    x = rng.standard_normal((rows, k)) * np.exp(rng.standard_normal((1, k)))
+    check_quantize(torch.from_numpy(x).to(TYPES[kind][0]).to(DEV), block_rows)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize_strided_and_unaligned_rows(kind, block_rows, rng):
+    base = torch.from_numpy(rng.standard_normal((40, 333))).to(TYPES[kind][0]).to(DEV)
+    check_quantize(base[:, 1:278], block_rows, ld_codes=320)
+    check_quantize(base[:20, :256], block_rows, ld_codes=256)
+    check_quantize(base[2:20:3, 5:6], block_rows, ld_codes=16)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize_special_values(block_rows, rng):
+    x = rng.standard_normal((20, 640)).astype(np.float32)
+    x[0, :128] = 0.0                       # an empty block
+    x[1, 5] = np.nan
+    x[2, 130] = -np.inf
+    x[3, :128] *= np.float32(1e38)         # no overflow on the way
+    x[4, :128] *= np.float32(1e-38)        # below the smallest scale
+    x[5, :128] *= np.float32(1e-28)
+    x[6, 256:384] = 448.0 * np.float32(2.0) ** np.arange(-64, 64)
+    x[7, 0] = np.float32(3.4e38)
+    x[8, :128] = (S.E4M3[np.arange(128) % 126] + S.E4M3[np.arange(128) % 126 + 1]) / 2
+    x[8, 0] = 448.0                        # scale 1: every value between two codes
+    for r in range(9, 20):
+        x[r, 128:256] = -0.0 if r % 2 else 1.0
+    check_quantize(torch.from_numpy(x).to(DEV), block_rows)
+
+
+def operands(rng, m, n, k, ld_a=None, ld_w=None):
+    def codes(rows, ld):
+        c = rng.integers(0, 256, (rows, ld or k), dtype=np.uint8)
+        c[:, :k][(c[:, :k] & 127) == 127] = 0x35            # NaN only past the rows' ends
+        return c
+    a, w = codes(m, ld_a), codes(n, ld_w)
+    kb = -(-k // 128)
+    sa = np.exp(rng.standard_normal((kb, m))).astype(np.float32)
+    sw = np.exp(rng.standard_normal((kb, -(-n // 128)))).astype(np.float32)
+    return a, sa, w, sw
+
+
+def dev(*arrays):
+    return [torch.from_numpy(x).to(DEV) for x in arrays]
+
+
+def check_product(rng, m, n, k, kind, ld_a=None, ld_w=None, ld_y=None, ws=None, offset=0):
+    a, sa, w, sw = operands(rng, m, n, k, ld_a, ld_w)
+    dtype, code, u = TYPES[kind]
+    d = P.f8_matmul_desc(m, n, k, code, ld_a, ld_w, ld_y)
+    ld = ld_y or n
+    y = torch.full((m * ld + offset,), -3.0, dtype=dtype, device=DEV)
+    P.ifq_f8_matmul(d, *dev(a, sa, w, sw), y[offset:], ws=ws)
+    got = y.double().cpu().numpy()
+    assert (got[:offset] == -3).all()
+    got = got[offset:].reshape(m, ld)
+    assert (got[:, n:] == -3).all()
+    want, size = S.f8_matmul(a[:, :k], sa, w[:, :k], sw)
+    kb = -(-k // 128)
+    bound = (128 + kb + 4) * 2.0 ** -23 * size + u * np.abs(want)
+    if kind == "f16":
+        big = np.abs(want) > 65000
+        want, got, bound = want[~big], got[:, :n][~big], bound[~big] + 2.0 ** -25
+    else:
+        got = got[:, :n]
+    worst = (np.abs(got - want) / bound).max() if want.size else 0.0
+    assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("m,n,k", [
+    (1, 1, 16), (1, 64, 128), (1, 1000, 512), (2, 129, 144), (5, 31, 1040), (16, 256, 256),
+    (17, 200, 4096), (33, 333, 2064), (64, 128, 640), (65, 257, 272), (128, 384, 1024),
+    (200, 130, 112), (257, 511, 400), (300, 1030, 1296)])
+def test_product(kind, m, n, k, rng):
+    check_product(rng, m, n, k, kind)
+
+
+@pytest.mark.parametrize("m,n,k,kind", [(1, 4096, 4096, "bf16"), (48, 2048, 8192, "f32"),
+                                        (512, 1024, 2048, "f16"), (1024, 768, 1040, "bf16")])
+def test_product_larger(m, n, k, kind, rng):
+    check_product(rng, m, n, k, kind)
+
+
+@pytest.mark.parametrize("m", [1, 7, 40, 150])
+def test_product_strides(m, rng):
+    check_product(rng, m, 77, 272, "bf16", ld_a=304, ld_w=288, ld_y=81)
+    check_product(rng, m, 128, 256, "f16", ld_a=512, ld_w=256, ld_y=136, offset=1)
+    check_product(rng, m, 130, 128, "f32", ld_y=131, offset=3)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 256, 4096), (30, 100, 2048), (600, 300, 512)])
+def test_product_same_bits_every_time(m, n, k, rng):
+    a, sa, w, sw = dev(*operands(rng, m, n, k))
+    d = P.f8_matmul_desc(m, n, k, P.IFQ_TYPE_F32)
+    ws = torch.zeros(max(1, P.ifq_f8_matmul_workspace_bytes(d)), dtype=torch.uint8, device=DEV)
+    outs = []
+    for i in range(4):
+        y = torch.empty(m, n, device=DEV)
+        P.ifq_f8_matmul(d, a, sa, w, sw, y, ws=ws if i % 2 else None)
+        outs.append(y)
+    assert all(torch.equal(outs[0], o) for o in outs[1:])
+
+
+def test_product_scale_nan_reaches_its_row(rng):
+    for m in (3, 70, 200):
+        a, sa, w, sw = operands(rng, m, 96, 384)
+        sa[1, 2] = np.nan
+        d = P.f8_matmul_desc(m, 96, 384, P.IFQ_TYPE_F32)
+        y = torch.empty(m, 96, device=DEV)
+        P.ifq_f8_matmul(d, *dev(a, sa, w, sw), y)
+        bad = torch.isnan(y)
+        assert bad[2].all() and bad.sum() == 96
+
+
+def test_product_of_quantized_matrices(rng):
+    """Both operands through the quantizer, an odd row length: the product is
+    that of the matrices up to half a step of 3 mantissa bits of every factor."""
+    m, n, k = 9, 150, 333
+    x = torch.from_numpy(rng.standard_normal((m, k))).to(torch.bfloat16).to(DEV)
+    w = torch.from_numpy(rng.standard_normal((n, k))).to(torch.bfloat16).to(DEV)
+    k16 = 336
+    a8 = torch.empty(m, k16, dtype=torch.uint8, device=DEV)
+    w8 = torch.empty(n, k16, dtype=torch.uint8, device=DEV)
+    sa, sw = torch.empty(3, m, device=DEV), torch.empty(3, 2, device=DEV)
+    P.ifq_f8_quantize(P.f8_quant_desc(m, k, P.IFQ_TYPE_BF16), x, a8, sa)
+    P.ifq_f8_quantize(P.f8_quant_desc(n, k, P.IFQ_TYPE_BF16, 128), w, w8, sw)
+    y = torch.empty(m, n, device=DEV)
+    P.ifq_f8_matmul(P.f8_matmul_desc(m, n, k16, P.IFQ_TYPE_F32), a8, sa, w8, sw, y)
+    xd, wd = x.double().cpu(), w.double().cpu()
+    # largest |x| of a block is 448 steps of scale; below, 2^-4 of the value or 2^-10 of the scale
+    tx = 2.0 ** -4 * xd.abs() + 2.0 ** -10 * xd.abs().max() / 448
+    tw = 2.0 ** -4 * wd.abs() + 2.0 ** -10 * wd.abs().max() / 448
+    bound = tx @ wd.abs().T + xd.abs() @ tw.T + tx @ tw.T
+    assert ((y.double().cpu() - xd @ wd.T).abs() <= bound).all()
+
+
+def test_product_on_another_stream(rng):
+    m, n, k = 4, 512, 4096
+    a, sa, w, sw = operands(rng, m, n, k)
+    d = P.f8_matmul_desc(m, n, k, P.IFQ_TYPE_F32)
+    da, dsa, dw, dsw = dev(a, sa, w, sw)
+    y0 = torch.empty(m, n, device=DEV)
+    P.ifq_f8_matmul(d, da, dsa, dw, dsw, y0)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    y1 = torch.zeros(m, n, device=DEV)
+    st.wait_stream(torch.cuda.current_stream())
+    P.ifq_f8_matmul(d, da, dsa, dw, dsw, y1, stream=st)
+    st.synchronize()
+    assert torch.equal(y0, y1)
