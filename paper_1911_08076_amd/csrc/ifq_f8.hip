@@ -7,8 +7,6 @@
 namespace ifq {
 namespace {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 // --- quantizer ----------------------------------------------------------------
@@ -170,6 +168,17 @@ void quantize(const QuantArgs& a, int block_rows, hipStream_t stream) {
 }
 
 // --- product --------------------------------------------------------------------
+//
+// The products go through the 16-bit matrix instructions, whose sums are
+// fp32: the 8-bit ones keep some 16 bits below the largest product (measured:
+// 1.5e-5 of the result's norm over 128 normal values, against 1e-8), which is
+// too few for a result in fp32. Every e4m3 value is a 16-bit float, and a
+// conversion of two codes is one instruction.
+//
+// The weights are the first operand and the activations the second: a lane's
+// sums then belong to one activation row, whose scale is one number, and the
+// weights' scale is the same for the whole wave. Every block of 128 is summed
+// from zero and added with the product of its scales.
 
 struct MatmulArgs {
   const uint8_t* a;
@@ -181,16 +190,8 @@ struct MatmulArgs {
   int32_t m, n, k, kb, nb;
 };
 
-// 32 bytes of a row's codes; zeros from k on.
-__device__ __forceinline__ v8i load32(const uint8_t* row, int c, int k) {
-  v4i lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-  if (c < k) lo = *reinterpret_cast<const v4i*>(row + c);
-  if (c + 16 < k) hi = *reinterpret_cast<const v4i*>(row + c + 16);
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-// Eight codes (two words) as 16-bit floats, which hold every e4m3 value.
-__device__ __forceinline__ f16x8 halves(int a, int b) {
+// Eight codes (two words) as 16-bit floats.
+__device__ __forceinline__ f16x8 halves(uint32_t a, uint32_t b) {
   const f16x2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
   const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
   const f16x2 z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
@@ -198,46 +199,282 @@ __device__ __forceinline__ f16x8 halves(int a, int b) {
   return f16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
-// 64 x 64 outputs per workgroup, 32 x 32 per wave: a lane of the weights'
-// operand holds 32 bytes of a column's row, one of the activations' the same
-// of an activation row, so a lane's sums all belong to one activation row and
-// take its scale as one number. Every block of 128 is summed from zero and
-// added with its scale. The products go through the 16-bit matrix
-// instructions, whose sums are fp32: the 8-bit ones keep some 16 bits below
-// the largest product (measured: 1.5e-5 of the result's norm over 128 normal
-// values, against 1e-8).
 template <typename T>
-__global__ __launch_bounds__(256) void f8_matmul(MatmulArgs a) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int r = lane & 31, h = lane >> 5;
-  const int n0 = blockIdx.x * 64 + (wave & 1) * 32, m0 = blockIdx.y * 64 + (wave >> 1) * 32;
-  if (n0 >= a.n || m0 >= a.m) return;
-  const int m = min(m0 + r, a.m - 1);
+__device__ __forceinline__ void store4(T* p, f32x4 v, bool vec, int left) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const t4 r = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+  if (vec && left >= 4) {
+    *reinterpret_cast<t4*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) p[i] = r[i];
+  }
+}
+
+// Whether rows of y can be written four elements at a time.
+template <typename T>
+__device__ __forceinline__ bool vectors(const MatmulArgs& a) {
+  return reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0 && a.ld_y % 4 == 0;
+}
+
+// Few activation rows: the weights are read once, and only the latency and
+// the memory's rate count. A workgroup takes 16 weight rows and 16 * MT
+// activation rows, its KS waves every KS-th block of 128; the waves' sums are
+// added in LDS in their order. A wave has the loads of AHEAD blocks in flight.
+template <typename T, int MT, int KS>
+__global__ __launch_bounds__(64 * KS) void f8_matmul_few(MatmulArgs a) {
+  constexpr int AHEAD = MT == 1 ? 4 : 2;
+  __shared__ __align__(16) float sums[KS][MT][64][4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
   const uint8_t* wrow = a.w + (int64_t)min(n0 + r, a.n - 1) * a.ld_w;
-  const uint8_t* arow = a.a + (int64_t)m * a.ld_a;
-  v16f acc = {};
-  for (int b = 0; b < a.kb; ++b) {
-    v16f part = {};
+  const uint8_t* arow[MT];
+  int m[MT];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int c = b * kF8Block + 64 * s + 32 * h;
-      const v8i wv = load32(wrow, c, a.k), av = load32(arow, c, a.k);
+  for (int x = 0; x < MT; ++x) {
+    m[x] = min(m0 + 16 * x + r, a.m - 1);
+    arow[x] = a.a + (int64_t)m[x] * a.ld_a;
+  }
+  const u32x4 zero = {0, 0, 0, 0};
+  u32x4 wv[AHEAD][2], av[AHEAD][MT][2];
+  float sa[AHEAD][MT], sw[AHEAD];
+  auto load = [&](int b, int to) {
 #pragma unroll
-      for (int t = 0; t < 8; t += 2)
-        part = __builtin_amdgcn_mfma_f32_32x32x16_f16(halves(wv[t], wv[t + 1]),
-                                                      halves(av[t], av[t + 1]), part, 0, 0, 0);
+    for (int c = 0; c < 2; ++c) {
+      const int k = b * kF8Block + 64 * c + 16 * g;
+      wv[to][c] = k < a.k ? *reinterpret_cast<const u32x4*>(wrow + k) : zero;
+#pragma unroll
+      for (int x = 0; x < MT; ++x)
+        av[to][x][c] = k < a.k ? *reinterpret_cast<const u32x4*>(arow[x] + k) : zero;
     }
-    const float s = a.sa[(int64_t)b * a.m + m] * a.sw[(int64_t)b * a.nb + n0 / kF8Block];
+    sw[to] = a.sw[(int64_t)b * a.nb + n0 / kF8Block];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = __builtin_fmaf(part[i], s, acc[i]);
-  }
-  if (m0 + r >= a.m) return;
-  T* y = static_cast<T*>(a.y) + (int64_t)m * a.ld_y;
+    for (int x = 0; x < MT; ++x) sa[to][x] = a.sa[(int64_t)b * a.m + m[x]];
+  };
+  f32x4 acc[MT];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int n = n0 + 8 * (i >> 2) + 4 * h + (i & 3);
-    if (n < a.n) y[n] = (T)acc[i];
+  for (int x = 0; x < MT; ++x) acc[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (wave + i * KS < a.kb) load(wave + i * KS, i);
+  for (int b0 = wave; b0 < a.kb; b0 += AHEAD * KS) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int b = b0 + i * KS;
+      if (b >= a.kb) break;
+      f32x4 part[MT];
+#pragma unroll
+      for (int x = 0; x < MT; ++x) part[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const f16x8 wh = halves(wv[i][c][e], wv[i][c][e + 1]);
+#pragma unroll
+          for (int x = 0; x < MT; ++x)
+            part[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                wh, halves(av[i][x][c][e], av[i][x][c][e + 1]), part[x], 0, 0, 0);
+        }
+#pragma unroll
+      for (int x = 0; x < MT; ++x) {
+        const float f = sa[i][x] * sw[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[x][e] = __builtin_fmaf(part[x][e], f, acc[x][e]);
+      }
+      if (b + AHEAD * KS < a.kb) load(b + AHEAD * KS, i);
+    }
   }
+#pragma unroll
+  for (int x = 0; x < MT; ++x) *reinterpret_cast<f32x4*>(sums[wave][x][lane]) = acc[x];
+  __syncthreads();
+  const bool vec = vectors<T>(a);
+  for (int i = threadIdx.x; i < 64 * MT; i += 64 * KS) {
+    const int x = i >> 6, l = i & 63, n = n0 + 4 * (l >> 4), mm = m0 + 16 * x + (l & 15);
+    f32x4 v = *reinterpret_cast<const f32x4*>(sums[0][x][l]);
+#pragma unroll
+    for (int w = 1; w < KS; ++w) v += *reinterpret_cast<const f32x4*>(sums[w][x][l]);
+    if (mm < a.m && n < a.n)
+      store4(static_cast<T*>(a.y) + (int64_t)mm * a.ld_y + n, v, vec, a.n - n);
+  }
+}
+
+// Sixteen zero bytes: what loads past the end of a row's codes read.
+__device__ const u32x4 g_zero16 = {0, 0, 0, 0};
+
+// 16 bytes per lane straight into LDS at dst (uniform) + 16 * lane: from a
+// pointer per lane, or from a uniform base and an offset per lane. The waits
+// for them are the caller's.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_lds16(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(dst), "v"(src) : "memory", "m0");
+}
+__device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(dst), "v"(off), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// A wave-uniform pointer that the compiler cannot tell for one.
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t*>((uintptr_t)((uint64_t)hi << 32 | lo));
+}
+
+// Many activation rows: a workgroup of WM x WN waves takes WM*MT*32 activation
+// and WN*NT*32 weight rows. The rows' 128 bytes of a block lie in LDS, two
+// blocks in turn, in 16-byte cells of which row r holds cell c at place
+// c ^ (r & 7), so that the lanes of a read spread over all banks.
+template <typename T, int MT, int NT, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a, int groups_m) {
+  constexpr int TM = WM * MT * 32, TN = WN * NT * 32, WAVES = WM * WN;
+  constexpr int LA = TM / 8 / WAVES, LW = TN / 8 / WAVES;   // loads of 8 rows, per wave
+  static_assert(TM % (8 * WAVES) == 0 && TN % (8 * WAVES) == 0, "");
+  __shared__ __align__(16) uint8_t lds[2][TM + TN][kF8Block];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  const int m0 = blockIdx.x % groups_m * TM, n0 = blockIdx.x / groups_m * TN;
+  const int wm = wave % WM * MT * 32, wn = wave / WM * NT * 32;
+  // A wave loads 8 * LA and 8 * LW rows: rows 8 i + lane / 8 from a base, at
+  // this lane's cell. Rows past the matrix repeat its last.
+  const int cell = 16 * ((lane & 7) ^ (lane >> 3));
+  const int a0 = min(m0 + 8 * LA * wave, a.m - 1), w0 = min(n0 + 8 * LW * wave, a.n - 1);
+  const uint8_t* abase = uniform(a.a + a0 * a.ld_a);
+  const uint8_t* wbase = uniform(a.w + w0 * a.ld_w);
+  uint32_t aoff[LA], woff[LW];
+#pragma unroll
+  for (int i = 0; i < LA; ++i)
+    aoff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.m - 1 - a0) * a.ld_a) + cell;
+#pragma unroll
+  for (int i = 0; i < LW; ++i)
+    woff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.n - 1 - w0) * a.ld_w) + cell;
+  const uint32_t to0 =
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0][0];
+  auto load = [&](int b) {
+    const uint32_t at = to0 + (b & 1) * (TM + TN) * kF8Block + 1024 * LA * wave;
+    const uint32_t wt = at + TM * kF8Block + 1024 * (LW - LA) * wave;
+    const uint8_t *ab = abase + b * kF8Block, *wb = wbase + b * kF8Block;
+    if ((b + 1) * kF8Block <= a.k) {
+#pragma unroll
+      for (int i = 0; i < LA; ++i) load_lds16(ab, aoff[i], at + 1024 * i);
+#pragma unroll
+      for (int i = 0; i < LW; ++i) load_lds16(wb, woff[i], wt + 1024 * i);
+    } else {
+      const bool past = b * kF8Block + cell >= a.k;
+      const void* zero = &g_zero16;
+#pragma unroll
+      for (int i = 0; i < LA; ++i) load_lds16(past ? zero : ab + aoff[i], at + 1024 * i);
+#pragma unroll
+      for (int i = 0; i < LW; ++i) load_lds16(past ? zero : wb + woff[i], wt + 1024 * i);
+    }
+  };
+  int m[MT];
+#pragma unroll
+  for (int x = 0; x < MT; ++x) m[x] = min(m0 + wm + 32 * x + r, a.m - 1);
+  const int nblock = min((n0 + wn) / kF8Block, a.nb - 1);
+  v16f acc[MT][NT];
+#pragma unroll
+  for (int x = 0; x < MT; ++x)
+#pragma unroll
+    for (int z = 0; z < NT; ++z) acc[x][z] = v16f{};
+  // the scales of a block come a block ahead, as its rows do
+  float sa[MT], sw;
+  auto load_scales = [&](int b) {
+    sw = a.sw[(int64_t)b * a.nb + nblock];
+#pragma unroll
+    for (int x = 0; x < MT; ++x) sa[x] = a.sa[(int64_t)b * a.m + m[x]];
+  };
+  load(0);
+  load_scales(0);
+  for (int b = 0; b < a.kb; ++b) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    float f[MT];
+#pragma unroll
+    for (int x = 0; x < MT; ++x) f[x] = sa[x] * sw;
+    if (b + 1 < a.kb) {
+      load(b + 1);
+      load_scales(b + 1);
+    }
+    const uint8_t(*at)[kF8Block] = lds[b & 1];
+    // a lane's cells: 2 j + h of its row
+    f16x8 wh[NT][8];
+#pragma unroll
+    for (int z = 0; z < NT; ++z)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(
+            &at[TM + wn + 32 * z + r][16 * ((2 * j + h) ^ (r & 7))]);
+        wh[z][2 * j] = halves(v[0], v[1]);
+        wh[z][2 * j + 1] = halves(v[2], v[3]);
+      }
+#pragma unroll
+    for (int x = 0; x < MT; ++x) {
+      v16f part[NT];
+#pragma unroll
+      for (int z = 0; z < NT; ++z) part[z] = v16f{};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(
+            &at[wm + 32 * x + r][16 * ((2 * j + h) ^ (r & 7))]);
+        const f16x8 a0 = halves(v[0], v[1]), a1 = halves(v[2], v[3]);
+#pragma unroll
+        for (int z = 0; z < NT; ++z) {
+          part[z] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wh[z][2 * j], a0, part[z], 0, 0, 0);
+          part[z] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wh[z][2 * j + 1], a1, part[z], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int z = 0; z < NT; ++z)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          acc[x][z][e] = __builtin_fmaf(part[z][e], f[x], acc[x][z][e]);
+    }
+  }
+  const bool vec = vectors<T>(a);
+#pragma unroll
+  for (int x = 0; x < MT; ++x) {
+    const int mm = m0 + wm + 32 * x + r;
+    if (mm >= a.m) continue;
+    T* y = static_cast<T*>(a.y) + (int64_t)mm * a.ld_y;
+#pragma unroll
+    for (int z = 0; z < NT; ++z)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = n0 + wn + 32 * z + 8 * e + 4 * h;
+        if (n < a.n)
+          store4(y + n, f32x4{acc[x][z][4 * e], acc[x][z][4 * e + 1], acc[x][z][4 * e + 2],
+                              acc[x][z][4 * e + 3]}, vec, a.n - n);
+      }
+  }
+}
+
+template <typename T, int MT>
+void few(const MatmulArgs& a, hipStream_t stream) {
+  const dim3 grid((a.n + 15) / 16, (a.m + 16 * MT - 1) / (16 * MT));
+  const int64_t groups = (int64_t)grid.x * grid.y;
+  if (MT < 4 && groups <= 128 && a.kb >= 16) {
+    if constexpr (MT < 4)
+      hipLaunchKernelGGL((f8_matmul_few<T, MT, 16>), grid, dim3(1024), 0, stream, a);
+  } else if (groups <= 512 && a.kb >= 8)
+    hipLaunchKernelGGL((f8_matmul_few<T, MT, 8>), grid, dim3(512), 0, stream, a);
+  else
+    hipLaunchKernelGGL((f8_matmul_few<T, MT, 4>), grid, dim3(256), 0, stream, a);
+}
+
+template <typename T>
+void matmul(const MatmulArgs& a, hipStream_t stream) {
+  if (a.m <= 16) return few<T, 1>(a, stream);
+  if (a.m <= 32) return few<T, 2>(a, stream);
+  if (a.m <= 64) return few<T, 4>(a, stream);
+  const int gm = (a.m + 127) / 128, gn = (a.n + 127) / 128;
+  hipLaunchKernelGGL((f8_matmul_tiled<T, 2, 2, 2, 2>), dim3(gm * gn), dim3(256), 0, stream, a,
+                     gm);
 }
 
 }  // namespace
@@ -279,13 +516,9 @@ hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a_, const f
   a.k = (int32_t)d.k;
   a.kb = (a.k + kF8Block - 1) / kF8Block;
   a.nb = (a.n + kF8Block - 1) / kF8Block;
-  const dim3 grid((a.n + 63) / 64, (a.m + 63) / 64);
-  if (d.y_type == IFQ_TYPE_BF16)
-    hipLaunchKernelGGL((f8_matmul<__bf16>), grid, dim3(256), 0, stream, a);
-  else if (d.y_type == IFQ_TYPE_F16)
-    hipLaunchKernelGGL((f8_matmul<_Float16>), grid, dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((f8_matmul<float>), grid, dim3(256), 0, stream, a);
+  if (d.y_type == IFQ_TYPE_BF16) matmul<__bf16>(a, stream);
+  else if (d.y_type == IFQ_TYPE_F16) matmul<_Float16>(a, stream);
+  else matmul<float>(a, stream);
   return hipGetLastError();
 }
 
