@@ -329,7 +329,9 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
 // Many activation rows: a workgroup of WM x WN waves takes WM*MT*32 activation
 // and WN*NT*32 weight rows. The rows' 128 bytes of a block lie in LDS, two
 // blocks in turn, in 16-byte cells of which row r holds cell c at place
-// c ^ (r & 7), so that the lanes of a read spread over all banks.
+// c ^ (r / 2 & 7): the 16 rows of which a read takes a cell each at a time
+// (lanes 0-3, 12-15, 20-27 and so on) then spread over all 64 banks. With
+// c ^ (r & 7) they met in pairs, 4 cycles for each read.
 template <typename T, int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a, int groups_m) {
   constexpr int TM = WM * MT * 32, TN = WN * NT * 32, WAVES = WM * WN;
@@ -341,18 +343,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
   const int m0 = blockIdx.x % groups_m * TM, n0 = blockIdx.x / groups_m * TN;
   const int wm = wave % WM * MT * 32, wn = wave / WM * NT * 32;
   // A wave loads 8 * LA and 8 * LW rows: rows 8 i + lane / 8 from a base, at
-  // this lane's cell. Rows past the matrix repeat its last.
-  const int cell = 16 * ((lane & 7) ^ (lane >> 3));
+  // this lane's cell (one for even i, one for odd). Rows past the matrix
+  // repeat its last.
+  static_assert(LA % 2 == 0 && LW % 2 == 0, "");
+  const int cells[2] = {16 * ((lane & 7) ^ (lane >> 4)), 16 * ((lane & 7) ^ (lane >> 4) ^ 4)};
   const int a0 = min(m0 + 8 * LA * wave, a.m - 1), w0 = min(n0 + 8 * LW * wave, a.n - 1);
   const uint8_t* abase = uniform(a.a + a0 * a.ld_a);
   const uint8_t* wbase = uniform(a.w + w0 * a.ld_w);
   uint32_t aoff[LA], woff[LW];
 #pragma unroll
   for (int i = 0; i < LA; ++i)
-    aoff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.m - 1 - a0) * a.ld_a) + cell;
+    aoff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.m - 1 - a0) * a.ld_a) + cells[i & 1];
 #pragma unroll
   for (int i = 0; i < LW; ++i)
-    woff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.n - 1 - w0) * a.ld_w) + cell;
+    woff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.n - 1 - w0) * a.ld_w) + cells[i & 1];
   const uint32_t to0 =
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0][0];
   auto load = [&](int b) {
@@ -365,12 +369,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
 #pragma unroll
       for (int i = 0; i < LW; ++i) load_lds16(wb, woff[i], wt + 1024 * i);
     } else {
-      const bool past = b * kF8Block + cell >= a.k;
+      const bool past[2] = {b * kF8Block + cells[0] >= a.k, b * kF8Block + cells[1] >= a.k};
       const void* zero = &g_zero16;
 #pragma unroll
-      for (int i = 0; i < LA; ++i) load_lds16(past ? zero : ab + aoff[i], at + 1024 * i);
+      for (int i = 0; i < LA; ++i) load_lds16(past[i & 1] ? zero : ab + aoff[i], at + 1024 * i);
 #pragma unroll
-      for (int i = 0; i < LW; ++i) load_lds16(past ? zero : wb + woff[i], wt + 1024 * i);
+      for (int i = 0; i < LW; ++i) load_lds16(past[i & 1] ? zero : wb + woff[i], wt + 1024 * i);
     }
   };
   int m[MT];
@@ -409,7 +413,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(
-            &at[TM + wn + 32 * z + r][16 * ((2 * j + h) ^ (r & 7))]);
+            &at[TM + wn + 32 * z + r][16 * ((2 * j + h) ^ (r >> 1 & 7))]);
         wh[z][2 * j] = halves(v[0], v[1]);
         wh[z][2 * j + 1] = halves(v[2], v[3]);
       }
@@ -421,7 +425,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(
-            &at[wm + 32 * x + r][16 * ((2 * j + h) ^ (r & 7))]);
+            &at[wm + 32 * x + r][16 * ((2 * j + h) ^ (r >> 1 & 7))]);
         const f16x8 a0 = halves(v[0], v[1]), a1 = halves(v[2], v[3]);
 #pragma unroll
         for (int z = 0; z < NT; ++z) {
