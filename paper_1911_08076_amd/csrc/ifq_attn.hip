@@ -39,6 +39,7 @@ struct AttnArgs {
   int32_t causal, window, sinks;
   float factor;         // scale * log2(e)
   int32_t row_blocks;   // blocks of a sequence's ratio * max_q query rows
+  FastDiv div_page;       // by the blocks of 32 tokens of a page
   int32_t splits, chunk;  // parts at most, and steps of a part at least
 };
 
@@ -120,12 +121,6 @@ __device__ __forceinline__ View view_of(const AttnArgs& a, int p_lo, int p_hi) {
   return v;
 }
 
-// Where, in the order of the view's blocks, those that hold positions up to p end.
-__device__ __forceinline__ int visible_end(const View& v, int p) {
-  return p < 0 ? 0 : p / kCodeTokens < v.first ? v.blocks
-                                                : v.sink_blocks + p / kCodeTokens - v.first + 1;
-}
-
 // A sequence's new tokens (queries) and cached tokens.
 struct Seq {
   int32_t row, count, length, pos;     // pos: position of the first query
@@ -142,14 +137,78 @@ __device__ __forceinline__ Seq seq_of(const KvArgs& c, int b) {
   return s;
 }
 
-// Running softmax and weighted sums of TILES x 16 query columns.
-template <int D, int TILES>
+// Running softmax and weighted sums of 16 query columns.
+template <int D>
 struct State {
-  f32x4 acc[TILES][D / 16];   // sums of factors * (16 + c): dims 16 x + 4g + r of a column
-  f32x4 wsum[TILES];          // sums of the factors, the same in every row
-  float m[TILES], mu[TILES];  // largest score so far, and the same or 0 where there is none
-  float l[TILES], ob[TILES];  // this lane's sums of p and of p * (o + 8 t)
+  f32x4 acc[D / 16];   // sums of factors * (16 + c): dims 16 x + 4g + r of a column
+  f32x4 wsum;          // sums of the factors, the same in every row
+  float m, mu;         // largest score so far, and the same or 0 where there is none
+  float l, ob;         // this lane's sums of p and of p * (o + 8 t)
+  float qc;            // factor * sum(q)
+  f32x4 init;          // -24 * sum(q)
+
+  template <typename X8>
+  __device__ __forceinline__ void begin(const X8 (&q)[D / 32], float factor) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += (float)q[i][e];
+    sum = sum_g(sum);
+    qc = sum * factor;
+    init = f32x4{-24.0f * sum, -24.0f * sum, -24.0f * sum, -24.0f * sum};
+    m = -__builtin_inff();
+    mu = l = ob = 0.0f;
+    wsum = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) acc[d] = f32x4{0, 0, 0, 0};
+  }
+
+  // Takes up eight scores (as differences to mu) of tokens with values' steps
+  // vt and middles vm: raises the maximum, adds to the sums and leaves the
+  // factors p * vt as two bfloat16 each.
+  __device__ __forceinline__ void take(float (&sc)[8], const float (&vt)[8],
+                                       const float (&vm)[8], u32x4& hi, u32x4& lo) {
+    float top = sc[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
+    // the maximum is raised only where a score passes it by 8 (a factor of
+    // 256 in p): sums keep their precision, and they are seldom rescaled
+    const float none = -__builtin_inff();
+    if (__ballot(top > (m == none ? none : 8.0f))) {
+      const float most = fmaxf(m, max_g(top) + mu);
+      const float mid = most == none ? 0.0f : most;
+      const float f = __builtin_amdgcn_exp2f(m - mid), by = mid - mu;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sc[e] -= by;
+      m = most;
+      mu = mid;
+      l *= f;
+      ob *= f;
+      wsum *= f;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) acc[d] *= f;
+    }
+    float fac[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f(sc[e]);
+      l += p;
+      ob = __builtin_fmaf(p, vm[e], ob);
+      fac[e] = p * vt[e];
+    }
+    split8(fac, hi, lo);
+    const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    const bf16x8 one = __builtin_bit_cast(bf16x8, ones);
+    wsum = Half<__bf16>::mfma(one, __builtin_bit_cast(bf16x8, hi), wsum);
+    wsum = Half<__bf16>::mfma(one, __builtin_bit_cast(bf16x8, lo), wsum);
+  }
 };
+
+// Whether the query at position pos sees position j.
+__device__ __forceinline__ bool sees(const AttnArgs& a, int pos, int j) {
+  return j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
+}
 
 // A block's place: its page's head (page 0 where the cache has no such page,
 // whose tokens are then hidden) and its first token there.
@@ -159,71 +218,85 @@ struct Place {
   bool held;
 };
 
-__device__ __forceinline__ Place place_of(const KvArgs& c, const View& view, int i, int id,
-                                          int64_t head_at, int per_page) {
-  Place p;
-  const int blk = view.block(i);
-  p.held = id >= 0 && id < c.num_pages;
-  p.head = c.cache + (p.held ? id : 0) * c.page_bytes + head_at;
-  p.tp = (per_page & (per_page - 1)) ? blk % per_page : blk & (per_page - 1);
-  p.tp *= kCodeTokens;
-  p.j0 = blk * kCodeTokens;
-  return p;
+// One sequence's pages of one head.
+struct Pages {
+  const int32_t* ids;
+  const uint8_t* cache;       // page 0's head
+  int64_t page_bytes;
+  FastDiv div;                // by the blocks of a page
+  int32_t per_page, num_pages;
+
+  __device__ __forceinline__ Pages(const AttnArgs& a, int b, int hk)
+      : ids(a.c.pages + (int64_t)b * a.c.max_pages),
+        cache(a.c.cache + hk * a.c.head_bytes),
+        page_bytes(a.c.page_bytes),
+        div(a.div_page),
+        per_page(a.c.page_tokens / kCodeTokens),
+        num_pages(a.c.num_pages) {}
+  __device__ __forceinline__ int page(int blk) const {
+    return (int)((__umulhi((uint32_t)blk, div.mul) + (uint32_t)blk) >> div.shift);
+  }
+  __device__ __forceinline__ int id(int blk) const { return ids[page(blk)]; }
+  __device__ __forceinline__ Place place(int blk, int id, bool there) const {
+    Place p;
+    const bool has = id >= 0 && id < num_pages;
+    p.head = cache + (has ? id : 0) * page_bytes;
+    p.tp = (blk - page(blk) * per_page) * kCodeTokens;
+    p.j0 = blk * kCodeTokens;
+    p.held = has && there;
+    return p;
+  }
+};
+
+// One of the N places, chosen by a number that is no constant: field by field
+// and by value, so that no array of places ends up in memory.
+template <typename V>
+__device__ __forceinline__ V choose(bool c, V a, V b) { return c ? a : b; }
+
+template <int N>
+__device__ __forceinline__ Place pick(const Place (&p)[N], int k) {
+  Place r = p[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    r.head = choose(k == i, p[i].head, r.head);
+    r.tp = choose(k == i, p[i].tp, r.tp);
+    r.j0 = choose(k == i, p[i].j0, r.j0);
+    r.held = choose(k == i, p[i].held, r.held);
+  }
+  return r;
 }
 
-// Runs steps i = begin, begin + step .. below end of the view over the query
+// Runs steps i = begin, begin + step .. below end of the view over 16 query
 // columns, U blocks (U * i ..) at a step: column n stands for query row
 // n % (16 / U) and sees only block n / (16 / U) of the U, so that with few
 // rows all columns take part in the softmax. pos: the position of this lane's
-// query in each tile. A step's loads are issued a step ahead: the keys' after
-// their last use, the values' likewise.
-template <typename T, int D, int U, int TILES>
+// query. A step's loads are issued a step ahead: the keys' after their last
+// use, the values' likewise.
+template <typename T, int D, int U>
 __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int b, int hk,
                                        int begin, int end, int step,
-                                       const typename Half<T>::x8 (&q)[TILES][D / 32],
-                                       const int (&pos)[TILES], int p_lo, int p_hi,
-                                       State<D, TILES>& s) {
+                                       const typename Half<T>::x8 (&q)[D / 32], int pos,
+                                       int p_lo, int p_hi, State<D>& s) {
   typedef Half<T> H;
-  static_assert(U == 1 || TILES == 1, "");
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int mine = n / (16 / U);          // the block of the U that this column sees
   const KvArgs& c = a.c;
-  float qc[TILES];      // factor * sum(q)
-  f32x4 init[TILES];    // -24 * sum(q)
-#pragma unroll
-  for (int x = 0; x < TILES; ++x) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += (float)q[x][i][e];
-    sum = sum_g(sum);
-    qc[x] = sum * a.factor;
-    init[x] = f32x4{-24.0f * sum, -24.0f * sum, -24.0f * sum, -24.0f * sum};
-    s.m[x] = -__builtin_inff();
-    s.mu[x] = s.l[x] = s.ob[x] = 0.0f;
-    s.wsum[x] = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) s.acc[x][d] = f32x4{0, 0, 0, 0};
-  }
+  s.begin(q, a.factor);
   if (begin >= end) return;
-  const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-  const int per_page = c.page_tokens / kCodeTokens;
-  const int32_t* table = c.pages + (int64_t)b * c.max_pages;
-  const int64_t head_at = hk * c.head_bytes;
+  const Pages pages(a, b, hk);
   const int last = view.blocks - 1;
 
   uint32_t kw[U][2][D / 32];
   u32x4 vw[U][D / 64], kp[2], vp[2];
   Place now[U], next[U];
-  auto find = [&](int i, Place* p) {
+  auto find = [&](int i, Place (&p)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = min(U * i + u, last);
-      p[u] = place_of(c, view, at, table[view.block(at) / per_page], head_at, per_page);
+      const int blk = view.block(min(U * i + u, last));
+      p[u] = pages.place(blk, pages.id(blk), U * i + u <= last);
     }
   };
-  auto load_keys = [&](const Place* p) {
+  auto load_keys = [&](const Place (&p)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -235,19 +308,13 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
       }
   };
   // the words of this column's tokens, of keys (part 0) or values
-  auto load_words = [&](const Place* p, int part, u32x4* to) {
-    const uint8_t* head = p[0].head;
-    int tp = p[0].tp;
-#pragma unroll
-    for (int u = 1; u < U; ++u) {
-      head = mine == u ? p[u].head : head;
-      tp = mine == u ? p[u].tp : tp;
-    }
-    const uint8_t* src = head + c.page_tokens * (D + 4 * part) + 4 * (tp + 4 * g);
+  auto load_words = [&](const Place (&p)[U], int part, u32x4 (&to)[2]) {
+    const Place at = pick(p, mine);
+    const uint8_t* src = at.head + c.page_tokens * (D + 4 * part) + 4 * (at.tp + 4 * g);
     to[0] = *reinterpret_cast<const u32x4*>(src);
     to[1] = *reinterpret_cast<const u32x4*>(src + 64);
   };
-  auto load_values = [&](const Place* p) {
+  auto load_values = [&](const Place (&p)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -262,123 +329,63 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
   load_values(now);
   load_words(now, 1, vp);
   for (int i = begin; i < end; i += step) {
-    const int ahead = min(i + step, end - 1);
-    find(ahead, next);
-    int j0 = now[0].j0;
-    bool held = now[0].held && U * i <= last;
+    find(min(i + step, end - 1), next);
+    const Place own = pick(now, mine);
     bool masked = false;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool there = now[u].held && U * i + u <= last;
-      masked |= !there || now[u].j0 + kCodeTokens - 1 > p_lo ||
+    for (int u = 0; u < U; ++u)
+      masked |= !now[u].held || now[u].j0 + kCodeTokens - 1 > p_lo ||
                 (a.window > 0 && now[u].j0 <= p_hi - a.window);
-      if (u > 0) {
-        j0 = mine == u ? now[u].j0 : j0;
-        held = mine == u ? there : held;
-      }
-    }
-    float sc[TILES][8];
+    float sc[8];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x4 d[TILES];
+      f32x4 d;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        f32x4 e[TILES];
+        f32x4 e = s.init;
 #pragma unroll
-        for (int x = 0; x < TILES; ++x) e[x] = init[x];
+        for (int w = 0; w < D / 32; ++w) e = H::mfma(codes8<H>(kw[u][t][w]), q[w], e);
 #pragma unroll
-        for (int w = 0; w < D / 32; ++w) {
-          const typename H::x8 k = codes8<H>(kw[u][t][w]);
-#pragma unroll
-          for (int x = 0; x < TILES; ++x) e[x] = H::mfma(k, q[x][w], e[x]);
-        }
-#pragma unroll
-        for (int x = 0; x < TILES; ++x)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) d[x][r] = u == 0 || mine == u ? e[x][r] : d[x][r];
+        for (int r = 0; r < 4; ++r) d[r] = u == 0 || mine == u ? e[r] : d[r];
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float st = row_step(kp[t][r]), o = row_offset(kp[t][r]);
-        const float f = st * a.factor, mid = __builtin_fmaf(8.0f, st, o);
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) sc[x][4 * t + r] = __builtin_fmaf(d[x][r], f, mid * qc[x]);
+        const float st = row_step(kp[t][r]), mid = __builtin_fmaf(8.0f, st, row_offset(kp[t][r]));
+        sc[4 * t + r] =
+            __builtin_fmaf(d[r], st * a.factor, __builtin_fmaf(mid, s.qc, -s.mu));
       }
     }
     load_keys(next);
     load_words(next, 0, kp);
-    float vt[8], vo[8];
+    float vt[8], vm[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       vt[e] = row_step(vp[e >> 2][e & 3]);
-      vo[e] = __builtin_fmaf(8.0f, vt[e], row_offset(vp[e >> 2][e & 3]));
+      vm[e] = __builtin_fmaf(8.0f, vt[e], row_offset(vp[e >> 2][e & 3]));
     }
-    u32x4 hi[TILES], lo[TILES];
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-      float tt[8], oo[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) tt[e] = vt[e], oo[e] = vo[e];
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = j0 + 16 * (e >> 2) + 4 * g + (e & 3);
-          const bool sees = held && j <= pos[x] &&
-                            (a.window == 0 || j > pos[x] - a.window || j < a.sinks);
-          sc[x][e] = sees ? sc[x][e] : -__builtin_inff();
-          // what a hidden row holds must not reach the sums, not even as 0 * NaN
-          tt[e] = sees ? tt[e] : 0.0f;
-          oo[e] = sees ? oo[e] : 0.0f;
-        }
-      }
-      float top = sc[x][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[x][e]);
-      // the maximum is raised only where a score passes it by 8 (a factor of
-      // 256 in p): sums keep their precision, and they are seldom rescaled
-      if (__ballot(top > s.m[x] + 8.0f)) {
-        const float m = fmaxf(s.m[x], max_g(top));
-        const float mu = m == -__builtin_inff() ? 0.0f : m;
-        const float f = __builtin_amdgcn_exp2f(s.m[x] - mu);
-        s.m[x] = m;
-        s.mu[x] = mu;
-        s.l[x] *= f;
-        s.ob[x] *= f;
-        s.wsum[x] *= f;
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) s.acc[x][d] *= f;
-      }
-      float fac[8];
+    if (masked) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(sc[x][e] - s.mu[x]);
-        s.l[x] += p;
-        s.ob[x] = __builtin_fmaf(p, oo[e], s.ob[x]);
-        fac[e] = p * tt[e];
+        const bool ok = own.held && sees(a, pos, own.j0 + 16 * (e >> 2) + 4 * g + (e & 3));
+        sc[e] = ok ? sc[e] : -__builtin_inff();
+        // what a hidden row holds must not reach the sums, not even as 0 * NaN
+        vt[e] = ok ? vt[e] : 0.0f;
+        vm[e] = ok ? vm[e] : 0.0f;
       }
-      split8(fac, hi[x], lo[x]);
-      const bf16x8 one = __builtin_bit_cast(bf16x8, ones);
-      s.wsum[x] = Half<__bf16>::mfma(one, __builtin_bit_cast(bf16x8, hi[x]), s.wsum[x]);
-      s.wsum[x] = Half<__bf16>::mfma(one, __builtin_bit_cast(bf16x8, lo[x]), s.wsum[x]);
     }
+    u32x4 hi, lo;
+    s.take(sc, vt, vm, hi, lo);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      bf16x8 fh[TILES], fl[TILES];
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        // block u counts for its own columns alone
-        const uint32_t keep = U == 1 || mine == u ? 0xFFFFFFFFu : 0u;
-        fh[x] = __builtin_bit_cast(bf16x8, hi[x] & keep);
-        fl[x] = __builtin_bit_cast(bf16x8, lo[x] & keep);
-      }
+      // block u counts for its own columns alone
+      const uint32_t keep = U == 1 || mine == u ? 0xFFFFFFFFu : 0u;
+      const bf16x8 fh = __builtin_bit_cast(bf16x8, hi & keep);
+      const bf16x8 fl = __builtin_bit_cast(bf16x8, lo & keep);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
         const bf16x8 v = codes8<Half<__bf16>>(vw[u][d >> 2][d & 3]);
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) {
-          s.acc[x][d] = Half<__bf16>::mfma(v, fh[x], s.acc[x][d]);
-          s.acc[x][d] = Half<__bf16>::mfma(v, fl[x], s.acc[x][d]);
-        }
+        s.acc[d] = Half<__bf16>::mfma(v, fh, s.acc[d]);
+        s.acc[d] = Half<__bf16>::mfma(v, fl, s.acc[d]);
       }
     }
     load_values(next);
@@ -386,11 +393,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
 #pragma unroll
     for (int u = 0; u < U; ++u) now[u] = next[u];
   }
-#pragma unroll
-  for (int x = 0; x < TILES; ++x) {
-    s.l[x] = sum_g(s.l[x]);
-    s.ob[x] = sum_g(s.ob[x]);
-  }
+  s.l = sum_g(s.l);
+  s.ob = sum_g(s.ob);
 }
 
 // Query row `row` of a sequence (row = token * ratio + head of the group) as
@@ -480,7 +484,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs& a, const Seq& s, int 
 // step of its part of the sequence for the same rows, and join their results
 // in LDS.
 template <typename T, int D, int U>
-__global__ __launch_bounds__(256) void kv_attention_few(AttnArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_few(AttnArgs a) {
   constexpr int ROWS = 16 / U, LD = D + 4;
   __shared__ __align__(16) float osum[4][16][LD];
   __shared__ float ml[4][16][2];
@@ -503,19 +507,19 @@ __global__ __launch_bounds__(256) void kv_attention_few(AttnArgs a) {
   const int chunk = max(a.chunk, (steps + a.splits - 1) / a.splits);
   const int parts = max(1, (steps + chunk - 1) / chunk);
   if (part >= parts) return;
-  typename Half<T>::x8 q[1][D / 32];
-  int pos[1];
-  load_row<T, D>(a, s, hk, row0 + n % ROWS, q[0], pos[0]);
-  State<D, 1> st;
-  attend<T, D, U, 1>(a, view, b, hk, part * chunk + wave, min(steps, (part + 1) * chunk), 4, q,
-                     pos, p_lo, p_hi, st);
-  const float corr = st.ob[0] - 24.0f * st.wsum[0][0];
+  typename Half<T>::x8 q[D / 32];
+  int pos;
+  load_row<T, D>(a, s, hk, row0 + n % ROWS, q, pos);
+  State<D> st;
+  attend<T, D, U>(a, view, b, hk, part * chunk + wave, min(steps, (part + 1) * chunk), 4, q, pos,
+                  p_lo, p_hi, st);
+  const float corr = st.ob - 24.0f * st.wsum[0];
 #pragma unroll
   for (int d = 0; d < D / 16; ++d)
-    *reinterpret_cast<f32x4*>(&osum[wave][n][16 * d + 4 * g]) = st.acc[0][d] + corr;
+    *reinterpret_cast<f32x4*>(&osum[wave][n][16 * d + 4 * g]) = st.acc[d] + corr;
   if (g == 0) {
-    ml[wave][n][0] = st.m[0];
-    ml[wave][n][1] = st.l[0];
+    ml[wave][n][0] = st.m;
+    ml[wave][n][1] = st.l;
   }
   __syncthreads();
   float* dst = parts > 1 ? a.part + (int64_t)(unit * a.splits + part) * ROWS * LD : nullptr;
@@ -544,63 +548,236 @@ __global__ __launch_bounds__(256) void kv_attention_few(AttnArgs a) {
   if (parts > 1) join_parts<T, D, ROWS>(a, s, unit, hk, row0, live, parts);
 }
 
-// Many query rows: each wave has TILES x 16 rows of its own and runs through
-// all that they see of the workgroup's part. The last rows, which see most,
-// come first.
-template <typename T, int D, int TILES>
-__global__ __launch_bounds__(256) void kv_attention_many(AttnArgs a) {
-  constexpr int WROWS = 16 * TILES, ROWS = 4 * WROWS, LD = D + 4;
+// The blocks of 32 tokens that many query rows take at a time, out of the
+// 4-bit codes: matrix operands of 16 bytes per lane, and each row's step and
+// middle, the keys' with the scores' factor.
+template <int D>
+struct Stage {
+  static constexpr int TOKENS = D == 64 ? 128 : 64, BLOCKS = TOKENS / kCodeTokens;
+  u32x4 k[TOKENS / 16][D / 32][64];
+  u32x4 v[BLOCKS][D / 16][64];
+  float kt[TOKENS], km[TOKENS], vt[TOKENS], vm[TOKENS];
+};
+
+// Many query rows: each wave has TILES x 16 of its own, and the workgroup
+// runs through all that its rows see of its part. The codes become operands
+// once for the workgroup, a quarter by each wave, in LDS, two stages in turn:
+// while one is computed on, the next one's codes are on their way into
+// registers. The last rows, which see most, come first.
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnArgs a) {
+  typedef Half<T> H;
+  typedef Half<__bf16> B;
+  typedef Stage<D> St;
+  constexpr int TILES = D == 256 ? 1 : 2;
+  constexpr int WROWS = 16 * TILES, ROWS = 4 * WROWS, LD = D + 4, NB = St::BLOCKS;
+  constexpr int KPW = St::TOKENS / 64, VPW = NB * (D / 64) / 4;  // key tiles, value chunks per wave
+  __shared__ __align__(16) St lds[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int unit = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
-  const int hk = unit % a.c.kv_heads;
-  const int rb = a.row_blocks - 1 - unit / a.c.kv_heads % a.row_blocks;
-  const int b = unit / a.c.kv_heads / a.row_blocks;
-  const Seq s = seq_of(a.c, b);
+  const KvArgs& c = a.c;
+  const int hk = unit % c.kv_heads;
+  const int rb = a.row_blocks - 1 - unit / c.kv_heads % a.row_blocks;
+  const int b = unit / c.kv_heads / a.row_blocks;
+  const Seq s = seq_of(c, b);
   const int rows = s.count * a.ratio;
   if (rb * ROWS >= rows) return;
-  // the split goes by what all of the workgroup's rows see
+  auto position = [&](int row) {
+    return a.causal ? min(s.pos + row / a.ratio, s.length - 1) : s.length - 1;
+  };
   const int live = min(ROWS, rows - rb * ROWS);
-  const int g_lo = a.causal ? min(s.pos + rb * ROWS / a.ratio, s.length - 1) : s.length - 1;
-  const int g_hi = a.causal ? min(s.pos + (rb * ROWS + live - 1) / a.ratio, s.length - 1)
-                            : s.length - 1;
-  const View all = view_of(a, g_lo, g_hi);
-  const int chunk = max(a.chunk, (all.blocks + a.splits - 1) / a.splits);
-  const int parts = max(1, (all.blocks + chunk - 1) / chunk);
+  const View view = view_of(a, position(rb * ROWS), position(rb * ROWS + live - 1));
+  const int steps = (view.blocks + NB - 1) / NB;
+  const int chunk = max(a.chunk, (steps + a.splits - 1) / a.splits);
+  const int parts = max(1, (steps + chunk - 1) / chunk);
   if (part >= parts) return;
+  const int begin = part * chunk, end = min(steps, begin + chunk);
   const int row0 = rb * ROWS + wave * WROWS;
-  const int own = min(WROWS, rows - row0);
-  if (own > 0) {
-    const int p_lo = a.causal ? min(s.pos + row0 / a.ratio, s.length - 1) : s.length - 1;
-    const int p_hi = a.causal ? min(s.pos + (row0 + own - 1) / a.ratio, s.length - 1)
-                              : s.length - 1;
-    typename Half<T>::x8 q[TILES][D / 32];
-    int pos[TILES];
+  const int own = min(WROWS, rows - row0);         // may be below 1: the wave only helps
+  const int p_lo = own > 0 ? position(row0) : 0;
+  const int p_hi = own > 0 ? position(row0 + own - 1) : -1;
+
+  typename H::x8 q[TILES][D / 32];
+  int pos[TILES];
+  State<D> st[TILES];
 #pragma unroll
-    for (int x = 0; x < TILES; ++x) load_row<T, D>(a, s, hk, row0 + 16 * x + n, q[x], pos[x]);
-    State<D, TILES> st;
-    attend<T, D, 1, TILES>(a, all, b, hk, part * chunk,
-                           min(min(all.blocks, (part + 1) * chunk), visible_end(all, p_hi)), 1, q,
-                           pos, p_lo, p_hi, st);
-    float* dst = parts > 1 ? a.part + ((int64_t)(unit * a.splits + part) * ROWS +
-                                       wave * WROWS) * LD : nullptr;
+  for (int x = 0; x < TILES; ++x) {
+    load_row<T, D>(a, s, hk, row0 + 16 * x + n, q[x], pos[x]);
+    st[x].begin(q[x], a.factor);
+  }
+
+  const Pages pages(a, b, hk);
+  const int last = view.blocks - 1;
+  auto block = [&](int step, int k) { return view.block(min(step * NB + k, last)); };
+  uint32_t kw[KPW][D / 32], kprm, vprm;
+  u32x4 vw[VPW];
+  auto load = [&](const Place (&p)[NB]) {
 #pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-      const int r = 16 * x + n;
-      if (r < own) {
-        const float corr = st.ob[x] - 24.0f * st.wsum[x][0];
-        if (parts > 1) {
+    for (int x = 0; x < KPW; ++x) {
+      const int t = wave * KPW + x;                // tile of 16 keys
+      const Place at = pick(p, t >> 1);
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(
+          at.head + (at.tp + 16 * (t & 1) + n) * (D / 2) + g * (D / 8));
 #pragma unroll
-          for (int d = 0; d < D / 16; ++d)
-            put_sums(dst + r * LD, 16 * d + 4 * g, st.acc[x][d] + corr);
-          if (g == 0) put_pair(dst + r * LD + D, st.m[x], st.l[x]);
-        } else {
-          const float f = st.l[x] == 0.0f ? 0.0f : 1.0f / st.l[x];
-          T* out = out_row<T, D>(a, s, hk, row0 + r) + 4 * g;
+      for (int w = 0; w < D / 32; ++w) kw[x][w] = src[w];
+    }
 #pragma unroll
-          for (int d = 0; d < D / 16; ++d) store4(out + 16 * d, (st.acc[x][d] + corr) * f);
+    for (int x = 0; x < VPW; ++x) {
+      const int t = wave * VPW + x;                // chunk of 32 values x 64 dims
+      const Place at = pick(p, t / (D / 64));
+      vw[x] = *reinterpret_cast<const u32x4*>(at.head + (c.page_tokens + at.tp) * (D / 2) +
+                                              t % (D / 64) * 1024 + lane * 16);
+    }
+    // a word of a key and of a value for each of the first TOKENS threads
+    const Place at = pick(p, (int)threadIdx.x / kCodeTokens % NB);
+    const uint32_t* prm =
+        reinterpret_cast<const uint32_t*>(at.head + c.page_tokens * D) + at.tp + (lane & 31);
+    kprm = prm[0];
+    vprm = prm[c.page_tokens];
+  };
+  auto stage = [&](St& to) {
+#pragma unroll
+    for (int x = 0; x < KPW; ++x)
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w)
+        to.k[wave * KPW + x][w][lane] = __builtin_bit_cast(u32x4, codes8<H>(kw[x][w]));
+#pragma unroll
+    for (int x = 0; x < VPW; ++x) {
+      const int t = wave * VPW + x;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        to.v[t / (D / 64)][t % (D / 64) * 4 + d][lane] =
+            __builtin_bit_cast(u32x4, codes8<B>(vw[x][d]));
+    }
+    if (threadIdx.x < St::TOKENS) {
+      const float t = row_step(kprm), u = row_step(vprm);
+      to.kt[threadIdx.x] = t * a.factor;
+      to.km[threadIdx.x] = __builtin_fmaf(8.0f, t, row_offset(kprm));
+      to.vt[threadIdx.x] = u;
+      to.vm[threadIdx.x] = __builtin_fmaf(8.0f, u, row_offset(vprm));
+    }
+  };
+
+  if (begin < end) {
+    Place now[NB], next[NB];
+    int id[NB];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int blk = block(begin, k);
+      now[k] = pages.place(blk, pages.id(blk), begin * NB + k <= last);
+      id[k] = pages.id(block(min(begin + 1, end - 1), k));
+    }
+    load(now);
+    stage(lds[begin & 1]);
+    __syncthreads();
+    for (int i = begin; i < end; ++i) {
+      const bool more = i + 1 < end;
+      if (more) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          next[k] = pages.place(block(i + 1, k), id[k], (i + 1) * NB + k <= last);
+          id[k] = pages.id(block(min(i + 2, end - 1), k));
+        }
+        load(next);
+      }
+      const St& from = lds[i & 1];
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        const int j0 = now[k].j0;
+        // blocks that none of the wave's rows sees
+        if (!now[k].held || j0 > p_hi ||
+            (a.window > 0 && j0 + kCodeTokens - 1 <= p_lo - a.window && j0 >= a.sinks))
+          continue;
+        const bool masked = j0 + kCodeTokens - 1 > p_lo ||
+                            (a.window > 0 && j0 <= p_hi - a.window);
+        float sc[TILES][8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          f32x4 d[TILES];
+#pragma unroll
+          for (int x = 0; x < TILES; ++x) d[x] = st[x].init;
+#pragma unroll
+          for (int w = 0; w < D / 32; ++w) {
+            const typename H::x8 kk =
+                __builtin_bit_cast(typename H::x8, from.k[2 * k + t][w][lane]);
+#pragma unroll
+            for (int x = 0; x < TILES; ++x) d[x] = H::mfma(kk, q[x][w], d[x]);
+          }
+          const int at = kCodeTokens * k + 16 * t + 4 * g;
+          const f32x4 kt = *reinterpret_cast<const f32x4*>(&from.kt[at]);
+          const f32x4 km = *reinterpret_cast<const f32x4*>(&from.km[at]);
+#pragma unroll
+          for (int x = 0; x < TILES; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              sc[x][4 * t + r] =
+                  __builtin_fmaf(d[x][r], kt[r], __builtin_fmaf(km[r], st[x].qc, -st[x].mu));
+        }
+        float vt[8], vm[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const int at = kCodeTokens * k + 4 * e + 4 * g;
+          const f32x4 t = *reinterpret_cast<const f32x4*>(&from.vt[at]);
+          const f32x4 o = *reinterpret_cast<const f32x4*>(&from.vm[at]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) vt[e + r] = t[r], vm[e + r] = o[r];
+        }
+        bf16x8 fh[TILES], fl[TILES];
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) {
+          float tt[8], oo[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) tt[e] = vt[e], oo[e] = vm[e];
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool ok = sees(a, pos[x], j0 + 16 * (e >> 2) + 4 * g + (e & 3));
+              sc[x][e] = ok ? sc[x][e] : -__builtin_inff();
+              tt[e] = ok ? tt[e] : 0.0f;         // not even 0 * NaN
+              oo[e] = ok ? oo[e] : 0.0f;
+            }
+          }
+          u32x4 hi, lo;
+          st[x].take(sc[x], tt, oo, hi, lo);
+          fh[x] = __builtin_bit_cast(bf16x8, hi);
+          fl[x] = __builtin_bit_cast(bf16x8, lo);
+        }
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          const bf16x8 v = __builtin_bit_cast(bf16x8, from.v[k][d][lane]);
+#pragma unroll
+          for (int x = 0; x < TILES; ++x) {
+            st[x].acc[d] = B::mfma(v, fh[x], st[x].acc[d]);
+            st[x].acc[d] = B::mfma(v, fl[x], st[x].acc[d]);
+          }
         }
       }
+      if (more) {
+        stage(lds[(i + 1) & 1]);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) now[k] = next[k];
+      }
+      __syncthreads();
+    }
+  }
+  float* dst = parts > 1 ? a.part + ((int64_t)(unit * a.splits + part) * ROWS +
+                                     wave * WROWS) * LD : nullptr;
+#pragma unroll
+  for (int x = 0; x < TILES; ++x) {
+    const int r = 16 * x + n;
+    const float sum = sum_g(st[x].l), corr = sum_g(st[x].ob) - 24.0f * st[x].wsum[0];
+    if (r >= own) continue;
+    if (parts > 1) {
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d)
+        put_sums(dst + r * LD, 16 * d + 4 * g, st[x].acc[d] + corr);
+      if (g == 0) put_pair(dst + r * LD + D, st[x].m, sum);
+    } else {
+      const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+      T* out = out_row<T, D>(a, s, hk, row0 + r) + 4 * g;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) store4(out + 16 * d, (st[x].acc[d] + corr) * f);
     }
   }
   if (parts > 1) join_parts<T, D, ROWS>(a, s, unit, hk, rb * ROWS, live, parts);
@@ -609,7 +786,6 @@ __global__ __launch_bounds__(256) void kv_attention_many(AttnArgs a) {
 // Which kernel, and how its work is split.
 struct Plan {
   int32_t few;            // blocks of a step for few rows (U), 0: many rows
-  int32_t tiles;          // tiles of 16 rows per wave, many rows
   int32_t row_blocks, splits, chunk;
   int64_t units;
   int32_t rows;           // per unit
@@ -619,8 +795,7 @@ Plan plan_of(const ifq_kv_desc& d) {
   Plan p;
   const int64_t rows = (int64_t)d.max_q * (d.heads / d.kv_heads);
   p.few = rows <= 4 && d.head_dim < 256 ? 4 : rows <= 8 ? 2 : rows <= 16 ? 1 : 0;
-  p.tiles = d.head_dim == 256 ? 1 : 2;
-  p.rows = p.few ? 16 / p.few : 64 * p.tiles;
+  p.rows = p.few ? 16 / p.few : d.head_dim == 256 ? 64 : 128;
   p.row_blocks = (int32_t)((rows + p.rows - 1) / p.rows);
   p.units = (int64_t)d.batch * d.kv_heads * p.row_blocks;
   // blocks that a unit may see, and steps of them
@@ -630,8 +805,9 @@ Plan plan_of(const ifq_kv_desc& d) {
                          (d.sinks + kCodeTokens - 1) / kCodeTokens + 1;
     blocks = std::min(blocks, seen);
   }
-  const int64_t steps = p.few ? (blocks + p.few - 1) / p.few : blocks;
-  const int64_t least = p.few ? 8 : 16;          // steps that are worth a workgroup
+  const int64_t at_once = p.few ? p.few : d.head_dim == 64 ? 4 : 2;
+  const int64_t steps = (blocks + at_once - 1) / at_once;
+  const int64_t least = 8;                       // steps that are worth a workgroup
   const int64_t want = std::max<int64_t>(1, kTargetGroups / p.units);
   int64_t chunk = std::max(least, (steps + want - 1) / want);
   if (p.few) chunk = (chunk + 3) / 4 * 4;
@@ -645,7 +821,6 @@ Plan plan_of(const ifq_kv_desc& d) {
 template <typename T, int D>
 hipError_t launch(const AttnArgs& a, const Plan& p, hipStream_t stream) {
   const dim3 grid((uint32_t)(p.units * p.splits)), block(256);
-  constexpr int TILES = D == 256 ? 1 : 2;
   if (p.few == 4) {
     if constexpr (D < 256)
       hipLaunchKernelGGL((kv_attention_few<T, D, 4>), grid, block, 0, stream, a);
@@ -654,7 +829,7 @@ hipError_t launch(const AttnArgs& a, const Plan& p, hipStream_t stream) {
   } else if (p.few == 1) {
     hipLaunchKernelGGL((kv_attention_few<T, D, 1>), grid, block, 0, stream, a);
   } else {
-    hipLaunchKernelGGL((kv_attention_many<T, D, TILES>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((kv_attention_many<T, D>), grid, block, 0, stream, a);
   }
   return hipGetLastError();
 }
@@ -693,6 +868,7 @@ hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs
   a.sinks = d.sinks;
   a.factor = d.scale * 1.4426950408889634f;
   a.row_blocks = p.row_blocks;
+  a.div_page = make_fastdiv((uint32_t)(d.page_tokens / kCodeTokens));
   a.splits = p.splits;
   a.chunk = p.chunk;
   if (p.units * p.splits > kMaxGroups) return hipErrorInvalidConfiguration;
