@@ -65,17 +65,27 @@ struct Half<_Float16> {
   }
 };
 
-// Eight codes of a word (nibble p + 4h: element 2p + h) as 16 + c.
+// What turns codes into 16 + c, kept in a scalar and a vector register: as
+// constants they would be two literals, and the and and the or two
+// instructions.
 template <typename H>
-__device__ __forceinline__ typename H::x8 codes8(uint32_t w) {
-  u32x4 r;
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int s = 4 * p - H::kAt;
-    r[p] = ((s < 0 ? w << -s : w >> s) & H::kMask) | H::kBase;
+struct Codes {
+  uint32_t mask, base;
+  __device__ __forceinline__ Codes() : mask(H::kMask), base(H::kBase) {
+    asm("" : "+s"(mask));
+    asm("" : "+v"(base));
   }
-  return __builtin_bit_cast(typename H::x8, r);
-}
+  // Eight codes of a word (nibble p + 4h: element 2p + h).
+  __device__ __forceinline__ typename H::x8 operator()(uint32_t w) const {
+    u32x4 r;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int s = 4 * p - H::kAt;
+      r[p] = ((s < 0 ? w << -s : w >> s) & mask) | base;
+    }
+    return __builtin_bit_cast(typename H::x8, r);
+  }
+};
 
 // Eight fp32 numbers as the sums of two bfloat16 each: the upper half of the
 // bits, and what remains, rounded.
@@ -146,6 +156,7 @@ struct State {
   float l, ob;         // this lane's sums of p and of p * (o + 8 t)
   float qc;            // factor * sum(q)
   f32x4 init;          // -24 * sum(q)
+  u32x4 ones;
 
   template <typename X8>
   __device__ __forceinline__ void begin(const X8 (&q)[D / 32], float factor) {
@@ -162,6 +173,8 @@ struct State {
     wsum = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) acc[d] = f32x4{0, 0, 0, 0};
+    ones = u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    asm("" : "+v"(ones));        // in registers: not made anew for each use
   }
 
   // Takes up eight scores (as differences to mu) of tokens with values' steps
@@ -198,7 +211,6 @@ struct State {
       fac[e] = p * vt[e];
     }
     split8(fac, hi, lo);
-    const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
     const bf16x8 one = __builtin_bit_cast(bf16x8, ones);
     wsum = Half<__bf16>::mfma(one, __builtin_bit_cast(bf16x8, hi), wsum);
     wsum = Half<__bf16>::mfma(one, __builtin_bit_cast(bf16x8, lo), wsum);
@@ -283,6 +295,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
   const KvArgs& c = a.c;
   s.begin(q, a.factor);
   if (begin >= end) return;
+  const Codes<H> kcodes;
+  const Codes<Half<__bf16>> vcodes;
   const Pages pages(a, b, hk);
   const int last = view.blocks - 1;
 
@@ -344,7 +358,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
       for (int u = 0; u < U; ++u) {
         f32x4 e = s.init;
 #pragma unroll
-        for (int w = 0; w < D / 32; ++w) e = H::mfma(codes8<H>(kw[u][t][w]), q[w], e);
+        for (int w = 0; w < D / 32; ++w) e = H::mfma(kcodes(kw[u][t][w]), q[w], e);
 #pragma unroll
         for (int r = 0; r < 4; ++r) d[r] = u == 0 || mine == u ? e[r] : d[r];
       }
@@ -383,7 +397,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
       const bf16x8 fl = __builtin_bit_cast(bf16x8, lo & keep);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
-        const bf16x8 v = codes8<Half<__bf16>>(vw[u][d >> 2][d & 3]);
+        const bf16x8 v = vcodes(vw[u][d >> 2][d & 3]);
         s.acc[d] = Half<__bf16>::mfma(v, fh, s.acc[d]);
         s.acc[d] = Half<__bf16>::mfma(v, fl, s.acc[d]);
       }
@@ -610,6 +624,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
   const Pages pages(a, b, hk);
   const int last = view.blocks - 1;
   auto block = [&](int step, int k) { return view.block(min(step * NB + k, last)); };
+  const Codes<H> kcodes;
+  const Codes<B> vcodes;
   uint32_t kw[KPW][D / 32], kprm, vprm;
   u32x4 vw[VPW];
   auto load = [&](const Place (&p)[NB]) {
@@ -641,14 +657,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
     for (int x = 0; x < KPW; ++x)
 #pragma unroll
       for (int w = 0; w < D / 32; ++w)
-        to.k[wave * KPW + x][w][lane] = __builtin_bit_cast(u32x4, codes8<H>(kw[x][w]));
+        to.k[wave * KPW + x][w][lane] = __builtin_bit_cast(u32x4, kcodes(kw[x][w]));
 #pragma unroll
     for (int x = 0; x < VPW; ++x) {
       const int t = wave * VPW + x;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
         to.v[t / (D / 64)][t % (D / 64) * 4 + d][lane] =
-            __builtin_bit_cast(u32x4, codes8<B>(vw[x][d]));
+            __builtin_bit_cast(u32x4, vcodes(vw[x][d]));
     }
     if (threadIdx.x < St::TOKENS) {
       const float t = row_step(kprm), u = row_step(vprm);
@@ -714,42 +730,37 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
               sc[x][4 * t + r] =
                   __builtin_fmaf(d[x][r], kt[r], __builtin_fmaf(km[r], st[x].qc, -st[x].mu));
         }
-        float vt[8], vm[8];
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          const int at = kCodeTokens * k + 4 * e + 4 * g;
-          const f32x4 t = *reinterpret_cast<const f32x4*>(&from.vt[at]);
-          const f32x4 o = *reinterpret_cast<const f32x4*>(&from.vm[at]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) vt[e + r] = t[r], vm[e + r] = o[r];
-        }
-        bf16x8 fh[TILES], fl[TILES];
+        u32x4 hi[TILES], lo[TILES];
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
-          float tt[8], oo[8];
+          // read anew for each tile, which changes them where it does not see
+          float vt[8], vm[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) tt[e] = vt[e], oo[e] = vm[e];
+          for (int e = 0; e < 8; e += 4) {
+            const int at = kCodeTokens * k + 4 * e + 4 * g;
+            const f32x4 t = *reinterpret_cast<const f32x4*>(&from.vt[at]);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(&from.vm[at]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vt[e + r] = t[r], vm[e + r] = o[r];
+          }
           if (masked) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const bool ok = sees(a, pos[x], j0 + 16 * (e >> 2) + 4 * g + (e & 3));
               sc[x][e] = ok ? sc[x][e] : -__builtin_inff();
-              tt[e] = ok ? tt[e] : 0.0f;         // not even 0 * NaN
-              oo[e] = ok ? oo[e] : 0.0f;
+              vt[e] = ok ? vt[e] : 0.0f;         // not even 0 * NaN
+              vm[e] = ok ? vm[e] : 0.0f;
             }
           }
-          u32x4 hi, lo;
-          st[x].take(sc[x], tt, oo, hi, lo);
-          fh[x] = __builtin_bit_cast(bf16x8, hi);
-          fl[x] = __builtin_bit_cast(bf16x8, lo);
+          st[x].take(sc[x], vt, vm, hi[x], lo[x]);
         }
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
           const bf16x8 v = __builtin_bit_cast(bf16x8, from.v[k][d][lane]);
 #pragma unroll
           for (int x = 0; x < TILES; ++x) {
-            st[x].acc[d] = B::mfma(v, fh[x], st[x].acc[d]);
-            st[x].acc[d] = B::mfma(v, fl[x], st[x].acc[d]);
+            st[x].acc[d] = B::mfma(v, __builtin_bit_cast(bf16x8, hi[x]), st[x].acc[d]);
+            st[x].acc[d] = B::mfma(v, __builtin_bit_cast(bf16x8, lo[x]), st[x].acc[d]);
           }
         }
       }
