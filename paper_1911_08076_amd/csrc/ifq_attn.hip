@@ -177,11 +177,8 @@ struct State {
     asm("" : "+v"(ones));        // in registers: not made anew for each use
   }
 
-  // Takes up eight scores (as differences to mu) of tokens with values' steps
-  // vt and middles vm: raises the maximum, adds to the sums and leaves the
-  // factors p * vt as two bfloat16 each.
-  __device__ __forceinline__ void take(float (&sc)[8], const float (&vt)[8],
-                                       const float (&vm)[8], u32x4& hi, u32x4& lo) {
+  // Raises the maximum for eight scores (as differences to mu).
+  __device__ __forceinline__ void raise(float (&sc)[8]) {
     float top = sc[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[e]);
@@ -202,6 +199,12 @@ struct State {
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) acc[d] *= f;
     }
+  }
+
+  // Adds the scores' tokens, with values' steps vt and middles vm, to the sums
+  // and leaves the factors p * vt as two bfloat16 each.
+  __device__ __forceinline__ void take(const float (&sc)[8], const float (&vt)[8],
+                                       const float (&vm)[8], u32x4& hi, u32x4& lo) {
     float fac[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -388,6 +391,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
       }
     }
     u32x4 hi, lo;
+    s.raise(sc);
     s.take(sc, vt, vm, hi, lo);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -649,8 +653,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
     const Place at = pick(p, (int)threadIdx.x / kCodeTokens % NB);
     const uint32_t* prm =
         reinterpret_cast<const uint32_t*>(at.head + c.page_tokens * D) + at.tp + (lane & 31);
-    kprm = prm[0];
-    vprm = prm[c.page_tokens];
+    // what no sequence wrote may be anything: it counts as 0
+    const bool there = at.held && at.j0 + (lane & 31) < s.length;
+    kprm = there ? prm[0] : 0u;
+    vprm = there ? prm[c.page_tokens] : 0u;
   };
   auto stage = [&](St& to) {
 #pragma unroll
@@ -668,10 +674,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
     }
     if (threadIdx.x < St::TOKENS) {
       const float t = row_step(kprm), u = row_step(vprm);
+      const float km = __builtin_fmaf(8.0f, t, row_offset(kprm));
+      const float vm = __builtin_fmaf(8.0f, u, row_offset(vprm));
+      // a value that is no number shows in its key's score instead, which a
+      // mask hides where a factor of 0 would not
+      const bool fine = vm - vm == 0.0f;
       to.kt[threadIdx.x] = t * a.factor;
-      to.km[threadIdx.x] = __builtin_fmaf(8.0f, t, row_offset(kprm));
-      to.vt[threadIdx.x] = u;
-      to.vm[threadIdx.x] = __builtin_fmaf(8.0f, u, row_offset(vprm));
+      to.km[threadIdx.x] = fine ? km : __builtin_nanf("");
+      to.vt[threadIdx.x] = fine ? u : 0.0f;
+      to.vm[threadIdx.x] = fine ? vm : 0.0f;
     }
   };
 
@@ -730,10 +741,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
               sc[x][4 * t + r] =
                   __builtin_fmaf(d[x][r], kt[r], __builtin_fmaf(km[r], st[x].qc, -st[x].mu));
         }
-        u32x4 hi[TILES], lo[TILES];
+        if (masked) {
+#pragma unroll
+          for (int x = 0; x < TILES; ++x)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (!sees(a, pos[x], j0 + 16 * (e >> 2) + 4 * g + (e & 3)))
+                sc[x][e] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int x = 0; x < TILES; ++x) st[x].raise(sc[x]);
+        // no branch from here on, so that a tile's products run beside the next
+        // tile's softmax
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
-          // read anew for each tile, which changes them where it does not see
           float vt[8], vm[8];
 #pragma unroll
           for (int e = 0; e < 8; e += 4) {
@@ -743,24 +764,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
 #pragma unroll
             for (int r = 0; r < 4; ++r) vt[e + r] = t[r], vm[e + r] = o[r];
           }
-          if (masked) {
+          u32x4 hi, lo;
+          st[x].take(sc[x], vt, vm, hi, lo);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool ok = sees(a, pos[x], j0 + 16 * (e >> 2) + 4 * g + (e & 3));
-              sc[x][e] = ok ? sc[x][e] : -__builtin_inff();
-              vt[e] = ok ? vt[e] : 0.0f;         // not even 0 * NaN
-              vm[e] = ok ? vm[e] : 0.0f;
-            }
-          }
-          st[x].take(sc[x], vt, vm, hi[x], lo[x]);
-        }
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, from.v[k][d][lane]);
-#pragma unroll
-          for (int x = 0; x < TILES; ++x) {
-            st[x].acc[d] = B::mfma(v, __builtin_bit_cast(bf16x8, hi[x]), st[x].acc[d]);
-            st[x].acc[d] = B::mfma(v, __builtin_bit_cast(bf16x8, lo[x]), st[x].acc[d]);
+          for (int d = 0; d < D / 16; ++d) {
+            const bf16x8 v = __builtin_bit_cast(bf16x8, from.v[k][d][lane]);
+            st[x].acc[d] = B::mfma(v, __builtin_bit_cast(bf16x8, hi), st[x].acc[d]);
+            st[x].acc[d] = B::mfma(v, __builtin_bit_cast(bf16x8, lo), st[x].acc[d]);
           }
         }
       }
