@@ -20,13 +20,15 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "ifq_serve.h"
 
 namespace ifq {
 namespace {
 
-constexpr int64_t kTargetGroups = 2048;   // workgroups that split work aims at
+constexpr double kSlots = 512;      // workgroups that run at once: two on a CU
+constexpr double kPartSteps = 32;   // cost of a part and of joining it, in steps
 
 struct AttnArgs {
   KvArgs c;
@@ -464,13 +466,31 @@ __device__ __forceinline__ void put_sums(float* row, int d, f32x4 o) {
   put_pair(row + d + 2, o[2], o[3]);
 }
 
-// Joins the parts of a unit's rows in their order, in the workgroup that
-// counts itself last. Called by all of a workgroup's threads after they have
-// written its part ([rows][D + 4]: sums, then m and l).
+// A row's result over some of its tokens: the largest score, the sum of p and
+// four of the sums of p * v, relative to that score.
+struct Result {
+  float m, l;
+  f32x4 o;
+  __device__ __forceinline__ void add(float m2, float l2, f32x4 o2) {
+    const float top = fmaxf(m, m2), mu = top == -__builtin_inff() ? 0.0f : top;
+    const float f = __builtin_amdgcn_exp2f(m - mu), f2 = __builtin_amdgcn_exp2f(m2 - mu);
+    l = f * l + f2 * l2;
+    o = f * o + f2 * o2;
+    m = top;
+  }
+};
+
+// Joins the parts of a unit's rows in the workgroup that counts itself last.
+// Called by all of a workgroup's threads after they have written its part
+// ([rows][D + 4]: sums, then m and l). Threads that rows and dims leave over
+// take a share of the parts each, eight of them in flight; the order of all
+// additions is the same in every call.
 template <typename T, int D, int ROWS>
 __device__ __forceinline__ void join_parts(const AttnArgs& a, const Seq& s, int unit, int hk,
                                            int row0, int live, int parts) {
+  constexpr int LD = D + 4, AHEAD = 8;
   __shared__ int last;
+  __shared__ Result share[256];
   // the part is in memory before the barrier, and so before the count
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -478,23 +498,40 @@ __device__ __forceinline__ void join_parts(const AttnArgs& a, const Seq& s, int 
     last = atomicInc(a.count + unit, (uint32_t)(parts - 1)) == (uint32_t)(parts - 1);
   __syncthreads();
   if (!last) return;
-  constexpr int LD = D + 4;
   const float* src = a.part + (int64_t)unit * a.splits * ROWS * LD;
-  for (int i = threadIdx.x; i < live * (D / 4); i += 256) {
-    const int r = i / (D / 4), d = i % (D / 4) * 4;
-    float m = -__builtin_inff(), l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
-    for (int p = 0; p < parts; ++p) {
-      const float* at = src + (int64_t)(p * ROWS + r) * LD;
-      const f32x2 ml = get_pair(at + D), x = get_pair(at + d), y = get_pair(at + d + 2);
-      const f32x4 v = {x[0], x[1], y[0], y[1]};
-      const float top = fmaxf(m, ml[0]), mu = top == -__builtin_inff() ? 0.0f : top;
-      const float f = __builtin_amdgcn_exp2f(m - mu), pf = __builtin_amdgcn_exp2f(ml[0] - mu);
-      l = f * l + pf * ml[1];
-      o = f * o + pf * v;
-      m = top;
+  const int items = live * (D / 4), shares = max(1, 256 / items);
+  for (int i0 = 0; i0 < items; i0 += 256) {
+    const int i = i0 + (int)threadIdx.x % (items < 256 ? items : 256);
+    const int mine = items < 256 ? (int)threadIdx.x / items : 0;
+    const bool on = i < items && mine < shares;
+    const int r = on ? i / (D / 4) : 0, d = on ? i % (D / 4) * 4 : 0;
+    Result all = {-__builtin_inff(), 0.0f, {0, 0, 0, 0}};
+    for (int p0 = on ? mine : parts; p0 < parts; p0 += AHEAD * shares) {
+      f32x2 ml[AHEAD], x[AHEAD], y[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const float* at = src + (int64_t)(min(p0 + k * shares, parts - 1) * ROWS + r) * LD;
+        ml[k] = get_pair(at + D);
+        x[k] = get_pair(at + d);
+        y[k] = get_pair(at + d + 2);
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (p0 + k * shares < parts)
+          all.add(ml[k][0], ml[k][1], f32x4{x[k][0], x[k][1], y[k][0], y[k][1]});
     }
-    store4(out_row<T, D>(a, s, hk, row0 + r) + d, o * (l == 0.0f ? 0.0f : 1.0f / l));
+    if (shares > 1) {
+      share[threadIdx.x] = all;
+      __syncthreads();
+      if (mine == 0)
+        for (int k = 1; k < shares; ++k) {
+          const Result& more = share[threadIdx.x + k * items];
+          all.add(more.m, more.l, more.o);
+        }
+    }
+    if (on && mine == 0)
+      store4(out_row<T, D>(a, s, hk, row0 + r) + d,
+             all.o * (all.l == 0.0f ? 0.0f : 1.0f / all.l));
   }
 }
 
@@ -828,12 +865,15 @@ Plan plan_of(const ifq_kv_desc& d) {
   }
   const int64_t at_once = p.few ? p.few : d.head_dim == 64 ? 4 : 2;
   const int64_t steps = (blocks + at_once - 1) / at_once;
-  const int64_t least = 8;                       // steps that are worth a workgroup
-  const int64_t want = std::max<int64_t>(1, kTargetGroups / p.units);
-  int64_t chunk = std::max(least, (steps + want - 1) / want);
-  if (p.few) chunk = (chunk + 3) / 4 * 4;
+  // With units * steps of work in parts of c steps over kSlots places, the parts'
+  // own cost (kPartSteps steps' time each) and the last part's length add up to
+  // units * steps * kPartSteps / (c * kSlots) + c, least at the root.
+  const double c = std::sqrt((double)p.units * (double)steps * kPartSteps / kSlots);
+  const int64_t parts = std::max<int64_t>(1, (int64_t)((double)steps / c + 0.5));
+  int64_t chunk = (steps + parts - 1) / parts;
+  if (p.few) chunk = (chunk + 3) / 4 * 4;      // the four waves take a step each
   p.chunk = (int32_t)chunk;
-  p.splits = (int32_t)std::max<int64_t>(1, (steps + chunk - 1) / chunk);
+  p.splits = (int32_t)((steps + chunk - 1) / chunk);
   // one arrival counter for each unit
   if (p.units * (int64_t)sizeof(uint32_t) > kSplitCounterBytes) p.splits = 1;
   return p;
