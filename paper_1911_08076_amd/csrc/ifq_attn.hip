@@ -445,22 +445,6 @@ __device__ __forceinline__ void store4(T* p, f32x4 v) {
   *reinterpret_cast<t4*>(p) = t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
 }
 
-// Parts go through memory between workgroups whose caches do not see one
-// another. Each number is written through to where all see it and read from
-// there (accesses of agent scope), so that no workgroup has to write back or
-// drop a whole cache for it: with fences around plain accesses 768 sequences
-// and heads in two parts each took 382 us instead of 74 unsplit.
-__device__ __forceinline__ void put_pair(float* p, float x, float y) {
-  const uint64_t v = f32_bits(x) | (uint64_t)f32_bits(y) << 32;
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED,
-                     __HIP_MEMORY_SCOPE_AGENT);
-}
-
-__device__ __forceinline__ f32x2 get_pair(const float* p) {
-  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
-                                                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
-
 __device__ __forceinline__ void put_sums(float* row, int d, f32x4 o) {
   put_pair(row + d, o[0], o[1]);
   put_pair(row + d + 2, o[2], o[3]);
@@ -491,13 +475,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs& a, const Seq& s, int 
   constexpr int LD = D + 4, AHEAD = 8;
   __shared__ int last;
   __shared__ Result share[256];
-  // the part is in memory before the barrier, and so before the count
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0)
-    last = atomicInc(a.count + unit, (uint32_t)(parts - 1)) == (uint32_t)(parts - 1);
-  __syncthreads();
-  if (!last) return;
+  if (!comes_last(a.count + unit, parts, &last)) return;
   const float* src = a.part + (int64_t)unit * a.splits * ROWS * LD;
   const int items = live * (D / 4), shares = max(1, 256 / items);
   for (int i0 = 0; i0 < items; i0 += 256) {

@@ -2,6 +2,8 @@
 // the product of two such matrices.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "ifq_serve.h"
 
 namespace ifq {
@@ -17,6 +19,7 @@ struct QuantArgs {
   float* scales;
   int64_t ld_x, ld_codes;
   int32_t rows, k, kb, rb;       // kb, rb: scale blocks along k and along the rows
+  int32_t wide;                  // workgroups along k
 };
 
 constexpr float kMinTop = 0x1p-96f;
@@ -91,8 +94,9 @@ template <typename T, bool VEC, int ROWS>
 __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
   constexpr int PER = ROWS == 16 ? 4 : 1;
   const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
-  const int row = ROWS == 16 ? blockIdx.y * 16 + g : blockIdx.y;
-  const int b0 = ROWS == 16 ? blockIdx.x * PER : blockIdx.x * 16 + g;
+  const int bx = blockIdx.x % a.wide, by = blockIdx.x / a.wide;
+  const int row = ROWS == 16 ? by * 16 + g : by;
+  const int b0 = ROWS == 16 ? bx * PER : bx * 16 + g;
   if (row >= a.rows) return;
   const T* src = static_cast<const T*>(a.x) + (int64_t)row * a.ld_x;
   uint8_t* dst = a.codes + (int64_t)row * a.ld_codes;
@@ -115,13 +119,14 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   __shared__ uint32_t part[4];
   const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
-  const int c = blockIdx.x * kF8Block + 8 * l;
+  const int bx = blockIdx.x % a.wide, by = blockIdx.x / a.wide;
+  const int c = bx * kF8Block + 8 * l;
   const int k16 = (a.k + 15) & ~15;
   float v[8][8];
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int row = blockIdx.y * kF8Block + 16 * i + g;
+    const int row = by * kF8Block + 16 * i + g;
     if (row < a.rows) {
       load8<T, VEC>(static_cast<const T*>(a.x) + (int64_t)row * a.ld_x, c, a.k, v[i]);
     } else {
@@ -139,32 +144,35 @@ __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   const float t = fmaxf(bits_f32(top), kMinTop);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int row = blockIdx.y * kF8Block + 16 * i + g;
+    const int row = by * kF8Block + 16 * i + g;
     if (row >= a.rows || c >= k16) continue;
     *reinterpret_cast<u32x2*>(a.codes + (int64_t)row * a.ld_codes + c) =
         codes8(v[i], t, top < kInfBits);
   }
-  if (threadIdx.x == 0) a.scales[(int64_t)blockIdx.x * a.rb + blockIdx.y] = scale_of(top);
+  if (threadIdx.x == 0) a.scales[(int64_t)bx * a.rb + by] = scale_of(top);
 }
 
 template <typename T, bool VEC>
-void quantize(const QuantArgs& a, int block_rows, hipStream_t stream) {
-  if (block_rows == 128) {
-    hipLaunchKernelGGL((f8_quantize_blocks<T, VEC>), dim3(a.kb, a.rb), dim3(256), 0, stream, a);
-  } else if (a.rows < 16) {
-    hipLaunchKernelGGL((f8_quantize_rows<T, VEC, 1>), dim3((a.kb + 15) / 16, a.rows), dim3(256),
-                       0, stream, a);
-  } else {
-    hipLaunchKernelGGL((f8_quantize_rows<T, VEC, 16>), dim3((a.kb + 3) / 4, (a.rows + 15) / 16),
-                       dim3(256), 0, stream, a);
-  }
+hipError_t quantize(QuantArgs a, int block_rows, hipStream_t stream) {
+  const bool one = block_rows == 1 && a.rows < 16;     // row by row
+  const int64_t high = block_rows == 128 ? a.rb : one ? a.rows : (a.rows + 15) / 16;
+  a.wide = block_rows == 128 ? a.kb : one ? (a.kb + 15) / 16 : (a.kb + 3) / 4;
+  if (a.wide * high > kMaxGroups) return hipErrorInvalidConfiguration;
+  const dim3 grid((uint32_t)(a.wide * high)), block(256);
+  if (block_rows == 128)
+    hipLaunchKernelGGL((f8_quantize_blocks<T, VEC>), grid, block, 0, stream, a);
+  else if (one)
+    hipLaunchKernelGGL((f8_quantize_rows<T, VEC, 1>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((f8_quantize_rows<T, VEC, 16>), grid, block, 0, stream, a);
+  return hipGetLastError();
 }
 
 template <typename T>
-void quantize(const QuantArgs& a, int block_rows, hipStream_t stream) {
+hipError_t quantize(const QuantArgs& a, int block_rows, hipStream_t stream) {
   const bool vec = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ld_x * sizeof(T) % 16 == 0;
-  if (vec) quantize<T, true>(a, block_rows, stream);
-  else quantize<T, false>(a, block_rows, stream);
+  return vec ? quantize<T, true>(a, block_rows, stream)
+             : quantize<T, false>(a, block_rows, stream);
 }
 
 // --- product --------------------------------------------------------------------
@@ -188,6 +196,9 @@ struct MatmulArgs {
   void* y;
   int64_t ld_a, ld_w, ld_y;
   int32_t m, n, k, kb, nb;
+  int32_t splits;          // of k, where tiles of 64 x 64 are few
+  uint32_t* count;
+  float* part;
 };
 
 // Eight codes (two words) as 16-bit floats.
@@ -340,7 +351,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
   __shared__ __align__(16) uint8_t lds[2][TM + TN][kF8Block];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-  const int m0 = blockIdx.x % groups_m * TM, n0 = blockIdx.x / groups_m * TN;
+  // this workgroup's tile, and blocks b0 .. b1-1 of k
+  constexpr bool SPLIT = MT * NT == 1;
+  const int splits = SPLIT ? a.splits : 1;
+  const int tile = SPLIT ? blockIdx.x / splits : blockIdx.x;
+  const int own = SPLIT ? blockIdx.x % splits : 0;
+  const int b0 = (int)((int64_t)a.kb * own / splits);
+  const int b1 = (int)((int64_t)a.kb * (own + 1) / splits);
+  const int m0 = tile % groups_m * TM, n0 = tile / groups_m * TN;
   const int wm = wave % WM * MT * 32, wn = wave / WM * NT * 32;
   // A wave loads 8 * LA and 8 * LW rows: rows 8 i + lane / 8 from a base, at
   // this lane's cell (one for even i, one for odd). Rows past the matrix
@@ -393,18 +411,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
 #pragma unroll
     for (int x = 0; x < MT; ++x) sa[x] = a.sa[(int64_t)b * a.m + m[x]];
   };
-  load(0);
-  load_scales(0);
-  for (int b = 0; b < a.kb; ++b) {
+  load(b0);
+  load_scales(b0);
+  for (int b = b0; b < b1; ++b) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     float f[MT];
 #pragma unroll
     for (int x = 0; x < MT; ++x) f[x] = sa[x] * sw;
-    if (b + 1 < a.kb) {
+    if (b + 1 < b1) {
       load(b + 1);
       load_scales(b + 1);
     }
+    // ahead of a wave of the other workgroup that still waits for its block
+    // (8192 x 14336 x 4096: 878 -> 852 us)
+    __builtin_amdgcn_s_setprio(1);
     const uint8_t(*at)[kF8Block] = lds[b & 1];
     // a lane's cells: 2 j + h of its row
     f16x8 wh[NT][8];
@@ -439,6 +460,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
         for (int e = 0; e < 16; ++e)
           acc[x][z][e] = __builtin_fmaf(part[z][e], f[x], acc[x][z][e]);
     }
+    __builtin_amdgcn_s_setprio(0);
+  }
+  if (SPLIT && splits > 1) {
+    // the parts go to memory lane by lane and are added in their order
+    __shared__ int last;
+    constexpr int SIZE = 64 * WAVES * 16;
+    float* mine = a.part + ((int64_t)tile * splits + own) * SIZE + threadIdx.x * 2;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2)
+      put_pair(mine + e * 64 * WAVES, acc[0][0][e], acc[0][0][e + 1]);
+    if (!comes_last(a.count + tile, splits, &last)) return;
+    const float* all = a.part + (int64_t)tile * splits * SIZE + threadIdx.x * 2;
+    acc[0][0] = v16f{};
+    for (int p = 0; p < splits; ++p)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const f32x2 v = get_pair(all + (int64_t)p * SIZE + e * 64 * WAVES);
+        acc[0][0][e] += v[0];
+        acc[0][0][e + 1] += v[1];
+      }
   }
   const bool vec = vectors<T>(a);
 #pragma unroll
@@ -462,23 +503,59 @@ template <typename T, int MT>
 void few(const MatmulArgs& a, hipStream_t stream) {
   const dim3 grid((a.n + 15) / 16, (a.m + 16 * MT - 1) / (16 * MT));
   const int64_t groups = (int64_t)grid.x * grid.y;
-  if (MT < 4 && groups <= 128 && a.kb >= 16) {
-    if constexpr (MT < 4)
-      hipLaunchKernelGGL((f8_matmul_few<T, MT, 16>), grid, dim3(1024), 0, stream, a);
-  } else if (groups <= 512 && a.kb >= 8)
+  if (groups <= 128 && a.kb >= 16)
+    hipLaunchKernelGGL((f8_matmul_few<T, MT, 16>), grid, dim3(1024), 0, stream, a);
+  else if (groups <= 512 && a.kb >= 8)
     hipLaunchKernelGGL((f8_matmul_few<T, MT, 8>), grid, dim3(512), 0, stream, a);
   else
     hipLaunchKernelGGL((f8_matmul_few<T, MT, 4>), grid, dim3(256), 0, stream, a);
 }
 
+template <typename T, int MT, int NT>
+void tiled(const MatmulArgs& a, hipStream_t stream) {
+  const int gm = (a.m + 64 * MT - 1) / (64 * MT), gn = (a.n + 64 * NT - 1) / (64 * NT);
+  hipLaunchKernelGGL((f8_matmul_tiled<T, MT, NT, 2, 2>), dim3(gm * gn * a.splits), dim3(256), 0,
+                     stream, a, gm);
+}
+
+// The kernel by the number of workgroups that each would have. Measured with
+// k = 4096 (us, the call's 5 included): 16 rows at a time in G workgroups
+// 6.1 (G = 63), 6.8 (252), 13.0 (768); 32 rows 7.8 (63), 8.3 (252), 14.1
+// (504), 24.7 (1024); tiles of 64 x 64 19 (up to 256), 49 (1024), 180 (4096);
+// of 128 x 128 36 (up to 256), 66 (512), 128 (1024).
+constexpr int64_t kSplitGroups = 512;    // workgroups that a split of k aims at
+
+enum Way { kRows16, kRows32, kTiles64, kTiles128 };
+
+int64_t tiles(int64_t m, int64_t n, int64_t tm, int64_t tn) {
+  return (m + tm - 1) / tm * ((n + tn - 1) / tn);
+}
+
+Way way_of(int64_t m, int64_t n) {
+  if (m <= 16 || tiles(m, n, 16, 16) <= 256) return kRows16;
+  if (m <= 64 || tiles(m, n, 32, 16) <= 512) return kRows32;
+  // a block of k on the busiest CU, in us: 0.18 + 0.35 for each tile of 64 x 64,
+  // 0.1 + 1.0 for each of 128 x 128
+  const double t64 = 0.18 + 0.35 * (double)((tiles(m, n, 64, 64) + 255) / 256);
+  const double t128 = 0.1 + (double)((tiles(m, n, 128, 128) + 255) / 256);
+  return t64 < t128 ? kTiles64 : kTiles128;
+}
+
+// Parts of k where tiles of 64 x 64 leave CUs idle: of 4 blocks at least.
+int64_t splits_of(int64_t m, int64_t n, int64_t k) {
+  if (way_of(m, n) != kTiles64) return 1;
+  const int64_t kb = (k + kF8Block - 1) / kF8Block, t = tiles(m, n, 64, 64);
+  return std::max<int64_t>(1, std::min(kSplitGroups / t, kb / 4));
+}
+
 template <typename T>
 void matmul(const MatmulArgs& a, hipStream_t stream) {
-  if (a.m <= 16) return few<T, 1>(a, stream);
-  if (a.m <= 32) return few<T, 2>(a, stream);
-  if (a.m <= 64) return few<T, 4>(a, stream);
-  const int gm = (a.m + 127) / 128, gn = (a.n + 127) / 128;
-  hipLaunchKernelGGL((f8_matmul_tiled<T, 2, 2, 2, 2>), dim3(gm * gn), dim3(256), 0, stream, a,
-                     gm);
+  switch (way_of(a.m, a.n)) {
+    case kRows16: return few<T, 1>(a, stream);
+    case kRows32: return few<T, 2>(a, stream);
+    case kTiles64: return tiled<T, 1, 1>(a, stream);
+    case kTiles128: return tiled<T, 2, 2>(a, stream);
+  }
 }
 
 }  // namespace
@@ -495,13 +572,25 @@ hipError_t launch_f8_quantize(const ifq_f8_quant_desc& d, const void* x, void* c
   a.k = (int32_t)d.k;
   a.kb = (int32_t)((d.k + kF8Block - 1) / kF8Block);
   a.rb = (int32_t)((d.rows + d.block_rows - 1) / d.block_rows);
-  if (d.x_type == IFQ_TYPE_BF16) quantize<__bf16>(a, d.block_rows, stream);
-  else if (d.x_type == IFQ_TYPE_F16) quantize<_Float16>(a, d.block_rows, stream);
-  else quantize<float>(a, d.block_rows, stream);
-  return hipGetLastError();
+  if (d.x_type == IFQ_TYPE_BF16) return quantize<__bf16>(a, d.block_rows, stream);
+  if (d.x_type == IFQ_TYPE_F16) return quantize<_Float16>(a, d.block_rows, stream);
+  return quantize<float>(a, d.block_rows, stream);
 }
 
-size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d) { return 0; }
+size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d) {
+  const int64_t s = splits_of(d.m, d.n, d.k);
+  return s == 1 ? 0 : kSplitCounterBytes + tiles(d.m, d.n, 64, 64) * s * 64 * 64 * sizeof(float);
+}
+
+int64_t f8_matmul_groups(const ifq_f8_matmul_desc& d) {
+  switch (way_of(d.m, d.n)) {
+    case kRows16: return tiles(d.m, d.n, 16, 16);
+    case kRows32: return tiles(d.m, d.n, 32, 16);
+    case kTiles64: return tiles(d.m, d.n, 64, 64) * splits_of(d.m, d.n, d.k);
+    case kTiles128: return tiles(d.m, d.n, 128, 128);
+  }
+  return 0;
+}
 
 hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a_, const float* a_scales,
                             const void* w, const float* w_scales, void* y, void* ws,
@@ -520,6 +609,11 @@ hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a_, const f
   a.k = (int32_t)d.k;
   a.kb = (a.k + kF8Block - 1) / kF8Block;
   a.nb = (a.n + kF8Block - 1) / kF8Block;
+  a.splits = (int32_t)splits_of(d.m, d.n, d.k);
+  a.count = static_cast<uint32_t*>(ws);
+  a.part = a.splits > 1
+               ? reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kSplitCounterBytes)
+               : nullptr;
   if (d.y_type == IFQ_TYPE_BF16) matmul<__bf16>(a, stream);
   else if (d.y_type == IFQ_TYPE_F16) matmul<_Float16>(a, stream);
   else matmul<float>(a, stream);

@@ -20,6 +20,8 @@ ifq_status fail(ifq_status st, const char* fmt, ...) {
 }
 
 ifq_status launched(hipError_t e, const char* what) {
+  if (e == hipErrorInvalidConfiguration)     // more workgroups than a launch may have
+    return fail(IFQ_ERR_UNSUPPORTED, "%s: too large for one launch", what);
   if (e != hipSuccess) return fail(IFQ_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
   return ifq::set_error(IFQ_OK, "");
 }
@@ -28,6 +30,7 @@ ifq_status launched(hipError_t e, const char* what) {
 // byte offsets are 64-bit throughout.
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxProductStride = (int64_t)1 << 25;
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -59,8 +62,10 @@ ifq_status check_matmul(const ifq_f8_matmul_desc* d) {
     return fail(IFQ_ERR_INVALID_ARGUMENT, "product: a leading dimension is below its row");
   if (d->k % 16 || d->ld_a % 16 || d->ld_w % 16)
     return fail(IFQ_ERR_UNSUPPORTED, "product: k, ld_a and ld_w must be multiples of 16");
-  // the launch grid: tiles of 32 rows and 16 columns at the least
-  if ((d->m + 31) / 32 * ((d->n + 15) / 16) > kMaxRows)
+  // 32-bit offsets within the rows of a tile
+  if (d->ld_a > kMaxProductStride || d->ld_w > kMaxProductStride)
+    return fail(IFQ_ERR_UNSUPPORTED, "product: ld_a and ld_w may be up to 2^25");
+  if (ifq::f8_matmul_groups(*d) > ifq::kMaxGroups)
     return fail(IFQ_ERR_UNSUPPORTED, "product: m x n is too large for one launch");
   return IFQ_OK;
 }

@@ -28,6 +28,7 @@ hipError_t launch_f8_quantize(const ifq_f8_quant_desc& d, const void* x, void* c
                               float* scales, hipStream_t stream);
 
 size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d);
+int64_t f8_matmul_groups(const ifq_f8_matmul_desc& d);   // workgroups of its launch
 hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a, const float* a_scales,
                             const void* w, const float* w_scales, void* y, void* ws,
                             hipStream_t stream);
@@ -58,6 +59,35 @@ __device__ __forceinline__ uint32_t f32_bits(float v) { return __builtin_bit_cas
 // Offset and step of a cached row, two bfloat16 in a word.
 __device__ __forceinline__ float row_offset(uint32_t w) { return bits_f32(w << 16); }
 __device__ __forceinline__ float row_step(uint32_t w) { return bits_f32(w & 0xFFFF0000u); }
+
+// Parts go through memory between workgroups whose caches do not see one
+// another. Each number is written through to where all see it and read from
+// there (accesses of agent scope), so that no workgroup has to write back or
+// drop a whole cache for it: with fences around plain accesses an attention of
+// 768 sequences and heads in two parts each took 382 us instead of 74 unsplit.
+__device__ __forceinline__ void put_pair(float* p, float x, float y) {
+  const uint64_t v = f32_bits(x) | (uint64_t)f32_bits(y) << 32;
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ f32x2 get_pair(const float* p) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
+                                                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// Counts a workgroup of `parts` that has written its part of a unit's result;
+// true in the one that comes last, which then may read all parts, and leaves
+// the counter at 0. Called by all threads; flag is in LDS.
+__device__ __forceinline__ bool comes_last(uint32_t* count, int parts, int* flag) {
+  // the part is in memory before the barrier, and so before the count
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    *flag = atomicInc(count, (uint32_t)(parts - 1)) == (uint32_t)(parts - 1);
+  __syncthreads();
+  return *flag != 0;
+}
 
 // x / d correctly rounded, given inv = 1 / d correctly rounded: the product
 // is within an ulp, and its remainder, exact in the fma, corrects it.

@@ -51,6 +51,15 @@ def test_quantize(kind, rows, k, block_rows, rng):
     check_quantize(torch.from_numpy(x).to(TYPES[kind][0]).to(DEV), block_rows)
 
 
+def test_quantize_many_rows(rng):
+    """More rows of workgroups than a second grid dimension would hold."""
+    x = torch.randn(65536 * 16 + 5, 3, device=DEV)
+    codes, scales = quantize(x)
+    some = rng.integers(0, len(codes), 500)
+    want, ws = S.f8_quantize(x[some].cpu().numpy())
+    assert np.array_equal(codes[some, :3], want) and np.array_equal(scales[:, some], ws)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_quantize_strided_and_unaligned_rows(kind, block_rows, rng):
@@ -130,6 +139,15 @@ def test_product(kind, m, n, k, rng):
                                         (512, 1024, 2048, "f16"), (1024, 768, 1040, "bf16")])
 def test_product_larger(m, n, k, kind, rng):
     check_product(rng, m, n, k, kind)
+
+
+@pytest.mark.parametrize("m,n,k,kind,more", [
+    (300, 700, 784, "bf16", {}), (517, 1100, 144, "f32", dict(ld_a=160, ld_w=192, ld_y=1101)),
+    (1000, 520, 256, "f16", dict(ld_y=528, offset=3)),          # tiles of 64
+    (2050, 1100, 272, "bf16", {}), (2300, 1030, 128, "f16", dict(ld_a=144, ld_y=1031)),
+    (4100, 530, 1040, "f32", dict(ld_w=1056, offset=1))])       # tiles of 128
+def test_product_tiles(m, n, k, kind, more, rng):
+    check_product(rng, m, n, k, kind, **more)
 
 
 @pytest.mark.parametrize("m", [1, 7, 40, 150])

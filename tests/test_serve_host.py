@@ -36,6 +36,16 @@ def test_quantize_refuses_descriptors(change, status):
     refused(status, P.ifq_f8_quantize, d, X, X, X)
 
 
+def test_launches_of_too_many_workgroups_are_refused():
+    refused(EUNSUP, P.ifq_f8_quantize, P.f8_quant_desc(2 ** 30, 2 ** 14, BF16), X, X, X)
+    d = kv(batch=65535, total_q=2 ** 30, max_q=2 ** 20, num_pages=1)
+    refused(EUNSUP, P.ifq_kv_append, d, X, X, X, None, None, X, X, X, X, X)
+    refused(EUNSUP, P.ifq_kv_read, d, X, X, X, X, X, X)
+    need = P.ifq_kv_attention_workspace_bytes(d)
+    assert need == 0
+    refused(EUNSUP, P.ifq_kv_attention, d, X, X, X, X, X, X)
+
+
 def test_quantize_refuses_pointers():
     d = P.f8_quant_desc(4, 64, BF16)
     for args in ((None, X, X), (X, None, X), (X, X, None), (ODD, X, X), (X, X[4:], X),
@@ -48,6 +58,8 @@ def test_quantize_refuses_pointers():
     (dict(m=-1), EINVAL), (dict(n=-1), EINVAL), (dict(k=0), EINVAL), (dict(n=2 ** 31), EINVAL),
     (dict(k=120), EUNSUP), (dict(ld_a=120), EINVAL), (dict(ld_a=136), EUNSUP),
     (dict(ld_w=127), EINVAL), (dict(ld_w=130), EUNSUP), (dict(ld_y=31), EINVAL),
+    (dict(ld_a=2 ** 25 + 16), EUNSUP), (dict(ld_w=2 ** 26), EUNSUP),
+    (dict(m=1, n=2 ** 30, ld_y=2 ** 30), EUNSUP),
     (dict(y_type=7), EINVAL), (dict(m=2 ** 30, n=2 ** 30, ld_y=2 ** 30), EUNSUP)])
 def test_product_refuses_descriptors(change, status):
     d = P.f8_matmul_desc(8, 32, 128, BF16)
