@@ -133,10 +133,14 @@ __device__ __forceinline__ uint32_t code_row(const float* x, uint32_t* code) {
     for (int i = 0; i < 8; ++i) code[i] = 0;
     return 0x7FC0u;                                          // NaN, step 0
   }
-  const bool flat = step == 0.0f;
+  // the quotients are those of a division; where the reciprocal and its products
+  // are far from the ends of fp32, div_by gives the same in three operations
+  const bool flat = step == 0.0f, plain = step > 0x1p-60f && step < 0x1p60f;
+  const float inv = 1.0f / step;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float c = flat ? 0.0f : (x[i] - off) / step;
+    const float d = x[i] - off;
+    const float c = plain ? div_by(d, step, inv) : flat ? 0.0f : d / step;
     code[i] = (uint32_t)fminf(fmaxf(__builtin_rintf(c), 0.0f), 15.0f);
   }
   return (o >> 16) | f32_bits(step);
@@ -186,12 +190,31 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
   uint32_t* words = reinterpret_cast<uint32_t*>(head);
   // new tokens of this block: lo .. hi-1
   const int lo = max(first - p0, 0), hi = min(end - p0, kCodeTokens);
+  // The values' words of this block: which nibbles are new, and the old words,
+  // asked for before the rows are coded. The old word is read in any case:
+  // with a branch for words of new tokens alone, the compiler stored through an
+  // index that the other lanes had not set.
+  uint32_t* vw = words + c.page_tokens * (D / 8) + tp * (D / 8);
+  const uint32_t fresh = hi > lo ? (0xFFFFFFFFu >> (32 - (hi - lo))) << lo : 0u;   // bit t: token t
+  constexpr int WORDS = 4 * D / 256;
+  uint32_t put[WORDS], old[WORDS];
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) {
+    const int i = threadIdx.x + 256 * k, g = (i >> 6) & 3;
+    put[k] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      put[k] |= ((fresh >> (16 * (e >> 2) + 4 * g + (e & 3))) & 1u) * 15u
+                << (4 * ((e >> 1) + 4 * (e & 1)));
+    old[k] = vw[i];
+  }
   for (int t0 = lo; t0 < hi; t0 += ROWS) {
     const int t = t0 + r;
     if (t < hi) {
       const int64_t row = s.row + (p0 + t - s.pos);
-      float x[8];
+      float x[8], v[8];
       uint32_t code[8];
+      load8(static_cast<const T*>(a.v) + row * a.v_stride + (int64_t)hk * D + 8 * l, v);
       load_rotated(a, static_cast<const T*>(a.k) + row * a.k_stride + (int64_t)hk * D, l, p0 + t,
                    x);
       uint32_t prm = code_row<L>(x, code);
@@ -200,8 +223,7 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
       for (int i = 0; i < 8; ++i) w |= code[i] << (4 * ((i >> 1) + 4 * (i & 1)));
       words[(tp + t) * (D / 8) + l] = w;
       if (l == 0) words[c.page_tokens * (D / 4) + tp + t] = prm;
-      load8(static_cast<const T*>(a.v) + row * a.v_stride + (int64_t)hk * D + 8 * l, x);
-      prm = code_row<L>(x, code);
+      prm = code_row<L>(v, code);
       if (l == 0) words[c.page_tokens * (D / 4) + c.page_tokens + tp + t] = prm;
       u32x2 bytes;
       bytes[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
@@ -210,22 +232,17 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
     }
   }
   __syncthreads();
-  uint32_t* vw = words + c.page_tokens * (D / 8) + tp * (D / 8);
-  // bit t: token t of the block is new
-  const uint32_t fresh = hi > lo ? (0xFFFFFFFFu >> (32 - (hi - lo))) << lo : 0u;
-  for (int i = threadIdx.x; i < 4 * D; i += 256) {
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) {
+    const int i = threadIdx.x + 256 * k;
     const int g = (i >> 6) & 3, n = (i >> 2) & 15, q = i & 3, dim = (i >> 8) * 64 + 16 * q + n;
-    uint32_t w = 0, put = 0;
+    uint32_t w = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int t = 16 * (e >> 2) + 4 * g + (e & 3);
-      const int at = 4 * ((e >> 1) + 4 * (e & 1));
-      w |= (uint32_t)(vcode[t][dim] & 15) << at;      // anything where t is not new
-      put |= ((fresh >> t) & 1u) * 15u << at;
+      w |= (uint32_t)(vcode[t][dim] & 15) << (4 * ((e >> 1) + 4 * (e & 1)));   // anything if old
     }
-    // the old word is read in any case: with a branch for words of new tokens
-    // alone, the compiler stored through an index that the other lanes had not set
-    if (put) vw[i] = (vw[i] & ~put) | (w & put);
+    if (put[k]) vw[i] = (old[k] & ~put[k]) | (w & put[k]);
   }
 }
 
