@@ -158,12 +158,17 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
     const int64_t i = (int64_t)(blockIdx.x - a.kv_groups) * ROWS + r;
     const int64_t t = i / c.heads;
     if (t >= c.total_q) return;
-    // the sequence of row t: the last whose first row is not after it
-    int lo = 0, hi = c.batch - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (c.offsets[mid] <= t) lo = mid;
-      else hi = mid - 1;
+    // the sequence of row t: the last whose first row is not after it; a row's
+    // lanes look at L sequences at a time (16 loads after one another, over
+    // 65535 sequences, would take longer than all else here)
+    int lo = 0;
+    for (int n = c.batch; n > 1;) {
+      const int step = (n + L - 1) / L;
+      const bool before = l * step < n && c.offsets[lo + l * step] <= t;
+      const uint64_t lanes = (__ballot(before) >> (threadIdx.x & 63 & ~(L - 1))) & ((1ull << L) - 1);
+      const int to = max(__popcll(lanes) - 1, 0) * step;
+      lo += to;
+      n = min(step, n - to);
     }
     const Span s = span_of(c, lo);
     if (t < s.row || t >= s.row + s.count) return;           // a row of no sequence
@@ -184,12 +189,22 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
   const int64_t from = (int64_t)(first & ~(kCodeTokens - 1)) + kCodeTokens * blk;
   if (from >= end) return;
   const int p0 = (int)from;
+  // new tokens of this block: lo .. hi-1
+  const int lo = max(first - p0, 0), hi = min(end - p0, kCodeTokens);
+  // A row's loads are on their way while its page is looked up, or the row
+  // before it coded.
+  float x[8], v[8];
+  auto fetch = [&](int t) {
+    if (t >= hi) return;
+    const int64_t row = s.row + (p0 + t - s.pos);
+    load8(static_cast<const T*>(a.v) + row * a.v_stride + (int64_t)hk * D + 8 * l, v);
+    load_rotated(a, static_cast<const T*>(a.k) + row * a.k_stride + (int64_t)hk * D, l, p0 + t, x);
+  };
   uint8_t* head = head_of(c, b, hk, p0);
+  fetch(lo + r);
   if (!head) return;
   const int tp = p0 % c.page_tokens;
   uint32_t* words = reinterpret_cast<uint32_t*>(head);
-  // new tokens of this block: lo .. hi-1
-  const int lo = max(first - p0, 0), hi = min(end - p0, kCodeTokens);
   // The values' words of this block: which nibbles are new, and the old words,
   // asked for before the rows are coded. The old word is read in any case:
   // with a branch for words of new tokens alone, the compiler stored through an
@@ -208,28 +223,21 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
                 << (4 * ((e >> 1) + 4 * (e & 1)));
     old[k] = vw[i];
   }
-  for (int t0 = lo; t0 < hi; t0 += ROWS) {
-    const int t = t0 + r;
-    if (t < hi) {
-      const int64_t row = s.row + (p0 + t - s.pos);
-      float x[8], v[8];
-      uint32_t code[8];
-      load8(static_cast<const T*>(a.v) + row * a.v_stride + (int64_t)hk * D + 8 * l, v);
-      load_rotated(a, static_cast<const T*>(a.k) + row * a.k_stride + (int64_t)hk * D, l, p0 + t,
-                   x);
-      uint32_t prm = code_row<L>(x, code);
-      uint32_t w = 0;
+  for (int t = lo + r; t < hi; t += ROWS) {
+    uint32_t code[8];
+    uint32_t prm = code_row<L>(x, code);
+    uint32_t w = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w |= code[i] << (4 * ((i >> 1) + 4 * (i & 1)));
-      words[(tp + t) * (D / 8) + l] = w;
-      if (l == 0) words[c.page_tokens * (D / 4) + tp + t] = prm;
-      prm = code_row<L>(v, code);
-      if (l == 0) words[c.page_tokens * (D / 4) + c.page_tokens + tp + t] = prm;
-      u32x2 bytes;
-      bytes[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-      bytes[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
-      *reinterpret_cast<u32x2*>(&vcode[t][8 * l]) = bytes;
-    }
+    for (int i = 0; i < 8; ++i) w |= code[i] << (4 * ((i >> 1) + 4 * (i & 1)));
+    words[(tp + t) * (D / 8) + l] = w;
+    if (l == 0) words[c.page_tokens * (D / 4) + tp + t] = prm;
+    prm = code_row<L>(v, code);
+    if (l == 0) words[c.page_tokens * (D / 4) + c.page_tokens + tp + t] = prm;
+    u32x2 bytes;
+    bytes[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+    bytes[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+    *reinterpret_cast<u32x2*>(&vcode[t][8 * l]) = bytes;
+    fetch(t + ROWS);
   }
   __syncthreads();
 #pragma unroll
