@@ -43,6 +43,11 @@ struct AttnArgs {
   int32_t row_blocks;   // blocks of a sequence's ratio * max_q query rows
   FastDiv div_page;       // by the blocks of 32 tokens of a page
   int32_t splits, chunk;  // parts at most, and steps of a part at least
+  // (sequence, row block, key/value head), the head fastest. A unit's parts are
+  // `units` workgroups apart: the last parts, which only the longest sequences
+  // have, would else fall to the same few XCDs (40 sequences of 100 to 5000
+  // tokens in 4 parts: 33.6 us side by side, 20.2 so)
+  int32_t units;
 };
 
 template <typename T>
@@ -523,7 +528,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_few(AttnAr
   __shared__ float ml[4][16][2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int unit = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
+  const int unit = blockIdx.x % a.units, part = blockIdx.x / a.units;
   const int hk = unit % a.c.kv_heads;
   const int rb = unit / a.c.kv_heads % a.row_blocks;
   const int b = unit / a.c.kv_heads / a.row_blocks;
@@ -608,7 +613,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
   __shared__ __align__(16) St lds[2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int unit = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
+  const int unit = blockIdx.x % a.units, part = blockIdx.x / a.units;
   const KvArgs& c = a.c;
   const int hk = unit % c.kv_heads;
   const int rb = a.row_blocks - 1 - unit / c.kv_heads % a.row_blocks;
@@ -847,7 +852,17 @@ Plan plan_of(const ifq_kv_desc& d) {
   // own cost (kPartSteps steps' time each) and the last part's length add up to
   // units * steps * kPartSteps / (c * kSlots) + c, least at the root.
   const double c = std::sqrt((double)p.units * (double)steps * kPartSteps / kSlots);
-  const int64_t parts = std::max<int64_t>(1, (int64_t)((double)steps / c + 0.5));
+  int64_t parts = std::max<int64_t>(1, (int64_t)((double)steps / c + 0.5));
+  // Few rows: at least a workgroup on each CU, as long as its waves have 128 x 128
+  // values each, since parts beside one another cost little more than one (16
+  // sequences of 1000 to 2100 tokens, 128 units: 16.6 us whole, 14.4 in two; one
+  // of 8000, 8 units: 11.8 in 8, 10.4 in 16; but one of 5000 with 64 dims 8.7 in
+  // 10, 9.6 in 20). From 32 on joining them takes what they save (8 units of 64000
+  // tokens: 21.8 us in 32, 24.1 in 64).
+  if (p.few) {
+    const int64_t worth = (steps * p.few * d.head_dim / 512 + 3) / 4;
+    parts = std::max(parts, std::min<int64_t>({(int64_t)kSlots / 2 / p.units, worth, 32}));
+  }
   int64_t chunk = (steps + parts - 1) / parts;
   if (p.few) chunk = (chunk + 3) / 4 * 4;      // the four waves take a step each
   p.chunk = (int32_t)chunk;
@@ -908,6 +923,7 @@ hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs
   a.factor = d.scale * 1.4426950408889634f;
   a.row_blocks = p.row_blocks;
   a.div_page = make_fastdiv((uint32_t)(d.page_tokens / kCodeTokens));
+  a.units = (int32_t)p.units;
   a.splits = p.splits;
   a.chunk = p.chunk;
   if (p.units * p.splits > kMaxGroups) return hipErrorInvalidConfiguration;
