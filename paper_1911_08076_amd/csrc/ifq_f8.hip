@@ -154,9 +154,15 @@ __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
 
 template <typename T, bool VEC>
 hipError_t quantize(QuantArgs a, int block_rows, hipStream_t stream) {
-  const bool one = block_rows == 1 && a.rows < 16;     // row by row
+  // Row by row where three quarters of its workgroups have work, or where rows
+  // are few (us, row by row and 16 rows at a time: 16 x 4096 2.8 and 4.4, 1024 x
+  // 14336 11.7 and 13.3, 8192 x 14336 72 and 75; but 8192 x 1000 10.1 and 9.3,
+  // 8192 x 128 7.8 and 4.3)
+  const int32_t per = (a.kb + 15) / 16;                // workgroups of a row
+  const bool one = block_rows == 1 && (int64_t)a.rows * per <= kMaxGroups &&
+                   (a.rows < 1024 || 4 * a.kb >= 3 * 16 * per);
   const int64_t high = block_rows == 128 ? a.rb : one ? a.rows : (a.rows + 15) / 16;
-  a.wide = block_rows == 128 ? a.kb : one ? (a.kb + 15) / 16 : (a.kb + 3) / 4;
+  a.wide = block_rows == 128 ? a.kb : one ? per : (a.kb + 3) / 4;
   if (a.wide * high > kMaxGroups) return hipErrorInvalidConfiguration;
   const dim3 grid((uint32_t)(a.wide * high)), block(256);
   if (block_rows == 128)

@@ -51,6 +51,16 @@ def test_quantize(kind, rows, k, block_rows, rng):
     check_quantize(torch.from_numpy(x).to(TYPES[kind][0]).to(DEV), block_rows)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,k", [(1023, 300), (1024, 300), (1030, 65), (1025, 1001),
+                                    (1100, 1500), (1024, 2050), (1041, 1537)])
+def test_quantize_long_and_narrow(kind, rows, k, rng):
+    """Many rows, of which some fill a workgroup and some do not."""
+    x = rng.standard_normal((rows, k)) * np.exp(rng.standard_normal((rows, 1)))
+    x[5, 3], x[rows - 1, k - 1], x[7] = np.nan, np.inf, 0.0
+    check_quantize(torch.from_numpy(x).to(TYPES[kind][0]).to(DEV))
+
+
 def test_quantize_many_rows(rng):
     """More rows of workgroups than a second grid dimension would hold."""
     x = torch.randn(65536 * 16 + 5, 3, device=DEV)
