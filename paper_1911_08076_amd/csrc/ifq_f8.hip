@@ -349,13 +349,18 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
 // c ^ (r / 2 & 7): the 16 rows of which a read takes a cell each at a time
 // (lanes 0-3, 12-15, 20-27 and so on) then spread over all 64 banks. With
 // c ^ (r & 7) they met in pairs, 4 cycles for each read.
-template <typename T, int MT, int NT, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a, int groups_m) {
+//
+// WK = 2: two such groups of waves in the workgroup take every other block of
+// k each, and the second's sums are added to the first's in LDS at the end.
+template <typename T, int MT, int NT, int WM, int WN, int WK>
+__global__ __launch_bounds__(64 * WM * WN * WK, 2) void f8_matmul_tiled(MatmulArgs a,
+                                                                        int groups_m) {
   constexpr int TM = WM * MT * 32, TN = WN * NT * 32, WAVES = WM * WN;
   constexpr int LA = TM / 8 / WAVES, LW = TN / 8 / WAVES;   // loads of 8 rows, per wave
   static_assert(TM % (8 * WAVES) == 0 && TN % (8 * WAVES) == 0, "");
-  __shared__ __align__(16) uint8_t lds[2][TM + TN][kF8Block];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __align__(16) uint8_t lds[WK * 2][TM + TN][kF8Block];
+  const int any = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = any % WAVES, half = any / WAVES;
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
   // this workgroup's tile, and blocks b0 .. b1-1 of k
   constexpr bool SPLIT = MT * NT == 1;
@@ -383,8 +388,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
     woff[i] = (uint32_t)(min(8 * i + (lane >> 3), a.n - 1 - w0) * a.ld_w) + cells[i & 1];
   const uint32_t to0 =
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0][0];
-  auto load = [&](int b) {
-    const uint32_t at = to0 + (b & 1) * (TM + TN) * kF8Block + 1024 * LA * wave;
+  auto load = [&](int b, int to) {
+    const uint32_t at = to0 + to * (TM + TN) * kF8Block + 1024 * LA * wave;
     const uint32_t wt = at + TM * kF8Block + 1024 * (LW - LA) * wave;
     const uint8_t *ab = abase + b * kF8Block, *wb = wbase + b * kF8Block;
     if ((b + 1) * kF8Block <= a.k) {
@@ -417,22 +422,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
 #pragma unroll
     for (int x = 0; x < MT; ++x) sa[x] = a.sa[(int64_t)b * a.m + m[x]];
   };
-  load(b0);
-  load_scales(b0);
-  for (int b = b0; b < b1; ++b) {
+  if (b0 + half < b1) {
+    load(b0 + half, 2 * half);
+    load_scales(b0 + half);
+  }
+  int turn = 0;
+  for (int b = b0 + half; b < b1 + half; b += WK, turn ^= 1) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     float f[MT];
 #pragma unroll
     for (int x = 0; x < MT; ++x) f[x] = sa[x] * sw;
-    if (b + 1 < b1) {
-      load(b + 1);
-      load_scales(b + 1);
+    if (WK > 1 && b >= b1) break;          // the last wait of a half with a block less
+    if (b + WK < b1) {
+      load(b + WK, 2 * half + (turn ^ 1));
+      load_scales(b + WK);
     }
     // ahead of a wave of the other workgroup that still waits for its block
     // (8192 x 14336 x 4096: 878 -> 852 us)
     __builtin_amdgcn_s_setprio(1);
-    const uint8_t(*at)[kF8Block] = lds[b & 1];
+    const uint8_t(*at)[kF8Block] = lds[2 * half + turn];
     // a lane's cells: 2 j + h of its row
     f16x8 wh[NT][8];
 #pragma unroll
@@ -467,6 +476,29 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void f8_matmul_tiled(MatmulArgs a,
           acc[x][z][e] = __builtin_fmaf(part[z][e], f[x], acc[x][z][e]);
     }
     __builtin_amdgcn_s_setprio(0);
+  }
+  if constexpr (WK > 1) {
+    static_assert(sizeof(lds) >= sizeof(float) * 64 * WAVES * MT * NT * 16, "");
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(&lds[0][0][0]) + (threadIdx.x & (64 * WAVES - 1));
+    if (half) {
+#pragma unroll
+      for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int z = 0; z < NT; ++z)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            sums[((x * NT + z) * 16 + e) * 64 * WAVES] = acc[x][z][e];
+    }
+    __syncthreads();
+    if (half) return;
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+      for (int z = 0; z < NT; ++z)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          acc[x][z][e] += sums[((x * NT + z) * 16 + e) * 64 * WAVES];
   }
   if (SPLIT && splits > 1) {
     // the parts go to memory lane by lane and are added in their order
@@ -517,11 +549,11 @@ void few(const MatmulArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((f8_matmul_few<T, MT, 4>), grid, dim3(256), 0, stream, a);
 }
 
-template <typename T, int MT, int NT>
+template <typename T, int MT, int NT, int WK>
 void tiled(const MatmulArgs& a, hipStream_t stream) {
   const int gm = (a.m + 64 * MT - 1) / (64 * MT), gn = (a.n + 64 * NT - 1) / (64 * NT);
-  hipLaunchKernelGGL((f8_matmul_tiled<T, MT, NT, 2, 2>), dim3(gm * gn * a.splits), dim3(256), 0,
-                     stream, a, gm);
+  hipLaunchKernelGGL((f8_matmul_tiled<T, MT, NT, 2, 2, WK>), dim3(gm * gn * a.splits),
+                     dim3(256 * WK), 0, stream, a, gm);
 }
 
 // The kernel by the number of workgroups that each would have. Measured with
@@ -559,8 +591,13 @@ void matmul(const MatmulArgs& a, hipStream_t stream) {
   switch (way_of(a.m, a.n)) {
     case kRows16: return few<T, 1>(a, stream);
     case kRows32: return few<T, 2>(a, stream);
-    case kTiles64: return tiled<T, 1, 1>(a, stream);
-    case kTiles128: return tiled<T, 2, 2>(a, stream);
+    case kTiles64: return tiled<T, 1, 1, 1>(a, stream);
+    case kTiles128:
+      // alone on its CU a tile waits for its blocks unless two of them are in
+      // hand: k in halves 515 x 6144 x 4096 43 -> 38 us, k = 1024 15.6 -> 14.9,
+      // k = 512 10.7 -> 11
+      if (tiles(a.m, a.n, 128, 128) <= 256 && a.kb >= 8) return tiled<T, 2, 2, 2>(a, stream);
+      return tiled<T, 2, 2, 1>(a, stream);
   }
 }
 

@@ -160,6 +160,16 @@ def test_product_tiles(m, n, k, kind, more, rng):
     check_product(rng, m, n, k, kind, **more)
 
 
+@pytest.mark.parametrize("m,n,k,kind,more", [
+    (4100, 1100, 272, "bf16", {}), (3500, 1500, 128, "f32", dict(ld_a=144, ld_y=1501)),
+    (4200, 1030, 1040, "f16", dict(ld_w=1056, offset=1)),       # more tiles of 128 than CUs
+    (1000, 3500, 16, "f32", {}), (900, 4000, 400, "bf16", dict(ld_a=416)),
+    (700, 5000, 2048, "f16", {}), (1030, 3501, 2064, "f32", dict(ld_w=2080)),
+    (530, 6000, 1040, "bf16", {})])                             # and fewer, k in halves
+def test_product_tiles_many_and_few(m, n, k, kind, more, rng):
+    check_product(rng, m, n, k, kind, **more)
+
+
 @pytest.mark.parametrize("m", [1, 7, 40, 150])
 def test_product_strides(m, rng):
     check_product(rng, m, 77, 272, "bf16", ld_a=304, ld_w=288, ld_y=81)
