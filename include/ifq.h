@@ -678,8 +678,9 @@ IFQ_API size_t ifq_static_workspace_bytes(void);
  * elements. All entry points below that take a stream are asynchronous on it,
  * allocate nothing and can be captured. Errors are the same throughout:
  * INVALID_ARGUMENT (a value out of its domain, a missing or misaligned
- * pointer), UNSUPPORTED (a size or alignment no kernel takes),
- * INSUFFICIENT_BUFFER (workspace), HIP.
+ * pointer), UNSUPPORTED (a size or alignment no kernel takes, or more work than
+ * one launch can hold: 2^24 - 1 workgroups), INSUFFICIENT_BUFFER (workspace),
+ * HIP.
  * ------------------------------------------------------------------------- */
 
 #define IFQ_TYPE_BF16 0
@@ -721,7 +722,8 @@ IFQ_API ifq_status ifq_f8_quantize(const ifq_f8_quant_desc* d, const void* x, vo
  * with sums in fp32, rounded once to y's type.
  *   m, n, k      k a multiple of 16 (a shorter row is filled up with zeros, as
  *                ifq_f8_quantize leaves it); m or n may be 0
- *   ld_a, ld_w   bytes from row to row, >= k, multiples of 16
+ *   ld_a, ld_w   bytes from row to row, >= k, multiples of 16 (UNSUPPORTED above
+ *                2^25)
  *   ld_y         elements from row to row of y, >= n
  *   y_type       IFQ_TYPE_BF16, F16 or F32
  */

@@ -87,9 +87,13 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
   return top >= kInfBits ? bits_f32(0x7FC00000u) : fmaxf(bits_f32(top), kMinTop) / 448.0f;
 }
 
-// A scale per row: 16 lanes hold a block of 128 values. ROWS = 16: a
+// A scale per row: 16 lanes hold a block of 128 values, read once and kept in
+// registers between the search for the largest and the coding. ROWS = 16: a
 // workgroup takes 16 rows x 4 blocks, so that the scales, which run along the
 // rows, are written 64 bytes at a time; ROWS = 1: 16 blocks of one row.
+// Bound by memory: 8192 x 14336 bfloat16 values 73 us, 4.9 TB/s (a copy of 4 GiB
+// reaches 4.64), with vector instructions on 81 % of the cycles; one row of 4096
+// takes 2.0 us on the GPU, the latency of a launch.
 template <typename T, bool VEC, int ROWS>
 __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
   constexpr int PER = ROWS == 16 ? 4 : 1;
@@ -114,7 +118,8 @@ __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
   }
 }
 
-// A scale per 128 x 128: a workgroup holds the block in registers.
+// A scale per 128 x 128: a workgroup holds the block in registers, 64 values to
+// a thread, so that it too is read once. For weights, when they are loaded.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   __shared__ uint32_t part[4];
@@ -239,6 +244,8 @@ __device__ __forceinline__ bool vectors(const MatmulArgs& a) {
 // the memory's rate count. A workgroup takes 16 weight rows and 16 * MT
 // activation rows, its KS waves every KS-th block of 128; the waves' sums are
 // added in LDS in their order. A wave has the loads of AHEAD blocks in flight.
+// 1 x 4096 x 4096: 5.8 us, of which the 16.8 MB of weights are 3.6 at the rate
+// of a copy and the rest is the launch and the first load's latency.
 template <typename T, int MT, int KS>
 __global__ __launch_bounds__(64 * KS) void f8_matmul_few(MatmulArgs a) {
   constexpr int AHEAD = MT == 1 ? 4 : 2;
@@ -349,6 +356,13 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
 // c ^ (r / 2 & 7): the 16 rows of which a read takes a cell each at a time
 // (lanes 0-3, 12-15, 20-27 and so on) then spread over all 64 banks. With
 // c ^ (r & 7) they met in pairs, 4 cycles for each read.
+//
+// Bound by the matrix instructions and the conversions beside them: 8192 x
+// 14336 x 4096 takes 860 to 930 us, 1.03 to 1.12 PFLOP/s (a bfloat16 product of
+// 8192^3 reaches 1.47 here), with products on 56 % and vector instructions on
+// 55 % of the cycles, at 1.7 GHz. Tiles of 128 x 128 on 4 waves: a wave converts
+// 128 rows' codes for 64 x 64 sums. 128 x 256 was equal, 192 x 256 and 256 x 256
+// spilled registers; three and four blocks in LDS were no faster than two.
 //
 // WK = 2: two such groups of waves in the workgroup take every other block of
 // k each, and the second's sums are added to the first's in LDS at the end.
