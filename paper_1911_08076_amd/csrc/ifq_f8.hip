@@ -244,7 +244,7 @@ __device__ __forceinline__ bool vectors(const MatmulArgs& a) {
 // the memory's rate count. A workgroup takes 16 weight rows and 16 * MT
 // activation rows, its KS waves every KS-th block of 128; the waves' sums are
 // added in LDS in their order. A wave has the loads of AHEAD blocks in flight.
-// 1 x 4096 x 4096: 5.8 us, of which the 16.8 MB of weights are 3.6 at the rate
+// 1 x 4096 x 4096: 5.7 us, of which the 16.8 MB of weights are 3.6 at the rate
 // of a copy and the rest is the launch and the first load's latency.
 template <typename T, int MT, int KS>
 __global__ __launch_bounds__(64 * KS) void f8_matmul_few(MatmulArgs a) {
@@ -359,8 +359,8 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
 //
 // Bound by the matrix instructions and the conversions beside them: 8192 x
 // 14336 x 4096 takes 860 to 930 us, 1.03 to 1.12 PFLOP/s (a bfloat16 product of
-// 8192^3 reaches 1.47 here), with products on 56 % and vector instructions on
-// 55 % of the cycles, at 1.7 GHz. Tiles of 128 x 128 on 4 waves: a wave converts
+// 8192^3 reaches 1.47 here), with products on 54 to 56 % and vector instructions on 53
+// to 55 % of the cycles, at 1.7 GHz. Tiles of 128 x 128 on 4 waves: a wave converts
 // 128 rows' codes for 64 x 64 sums. 128 x 256 was equal, 192 x 256 and 256 x 256
 // spilled registers; three and four blocks in LDS were no faster than two.
 //
