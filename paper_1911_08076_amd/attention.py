@@ -27,7 +27,8 @@ def rotation_tables(positions, rot_dim, base=10000.0, device="cuda"):
 class _Workspace:
     """One zero-filled device workspace for calls that follow one another, made
     larger when a call needs more. Smaller ones are kept, since a captured graph
-    may hold them: sizes double, so together they are below the largest."""
+    may hold them: sizes double, so together they are below the largest. A call
+    under capture that needs a larger one gets one of the graph's own."""
 
     def __init__(self):
         self._all = []
@@ -35,6 +36,10 @@ class _Workspace:
     def get(self, nbytes, device):
         if not nbytes:
             return None
+        if torch.cuda.is_current_stream_capturing():
+            # filled at every replay, not now: for the graph alone
+            if not self._all or self._all[-1].numel() < nbytes:
+                return torch.zeros(nbytes, dtype=torch.uint8, device=device)
         if not self._all or self._all[-1].numel() < nbytes:
             most = 2 * self._all[-1].numel() if self._all else 0
             self._all.append(torch.zeros(max(nbytes, most), dtype=torch.uint8, device=device))

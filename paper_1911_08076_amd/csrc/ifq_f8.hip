@@ -359,10 +359,11 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
 //
 // Bound by the matrix instructions and the conversions beside them: 8192 x
 // 14336 x 4096 takes 860 to 930 us, 1.03 to 1.12 PFLOP/s (a bfloat16 product of
-// 8192^3 reaches 1.47 here), with products on 54 to 56 % and vector instructions on 53
-// to 55 % of the cycles, at 1.7 GHz. Tiles of 128 x 128 on 4 waves: a wave converts
-// 128 rows' codes for 64 x 64 sums. 128 x 256 was equal, 192 x 256 and 256 x 256
-// spilled registers; three and four blocks in LDS were no faster than two.
+// 8192^3 reaches 1.47 here), with products on 54 to 56 % and vector instructions
+// on 53 to 55 % of the cycles, at 1.7 GHz. Tiles of 128 x 128 on 4 waves: a wave
+// converts 128 rows' codes for 64 x 64 sums. 128 x 256 was equal, 192 x 256 and
+// 256 x 256 spilled registers; three and four blocks in LDS were no faster than
+// two.
 //
 // WK = 2: two such groups of waves in the workgroup take every other block of
 // k each, and the second's sums are added to the first's in LDS at the end.

@@ -172,7 +172,8 @@ __global__ __launch_bounds__(256) void kv_append(AppendArgs a) {
     for (int n = c.batch; n > 1;) {
       const int step = (n + L - 1) / L;
       const bool before = l * step < n && c.offsets[lo + l * step] <= t;
-      const uint64_t lanes = (__ballot(before) >> (threadIdx.x & 63 & ~(L - 1))) & ((1ull << L) - 1);
+      const uint64_t lanes =
+          (__ballot(before) >> (threadIdx.x & 63 & ~(L - 1))) & ((1ull << L) - 1);
       const int to = max(__popcll(lanes) - 1, 0) * step;
       lo += to;
       n = min(step, n - to);

@@ -156,6 +156,31 @@ def test_nothing_new_and_a_captured_step():
             torch.cuda.synchronize()
 
 
+def test_first_step_under_capture():
+    """A workspace that a capture makes is zero at its replays only: an eager step
+    between capture and replay, and the replays after it, are right."""
+    layer, w1, w2, g = make(num_pages=64, max_pages=64)
+    other = make(num_pages=64, max_pages=64)[0]
+    x = torch.randn(1500, 272, generator=g, device=DEV).to(torch.bfloat16)
+    pages = torch.arange(64, dtype=torch.int32, device=DEV).view(1, 64)
+    args = i32([0, 1]), i32([1501]), pages
+    token = torch.randn(1, 272, generator=g, device=DEV).to(torch.bfloat16)
+    other(x, i32([0, 1500]), i32([1500]), pages, max_q=1500)
+    want = other(token, *args, max_q=1)
+    assert other.workspace._all            # the step is one that needs a workspace
+    layer.cache.copy_(other.cache)
+    out = torch.empty_like(token)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer(token, *args, max_q=1, out=out)
+    assert torch.equal(layer(token, *args, max_q=1), want)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want)
+        assert torch.equal(layer(token, *args, max_q=1), want)
+
+
 def test_example_runs(capsys):
     import importlib.util
     import os
