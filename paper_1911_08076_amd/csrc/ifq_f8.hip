@@ -571,11 +571,6 @@ void tiled(const MatmulArgs& a, hipStream_t stream) {
                      dim3(256 * WK), 0, stream, a, gm);
 }
 
-// The kernel by the number of workgroups that each would have. Measured with
-// k = 4096 (us, the call's 5 included): 16 rows at a time in G workgroups
-// 6.1 (G = 63), 6.8 (252), 13.0 (768); 32 rows 7.8 (63), 8.3 (252), 14.1
-// (504), 24.7 (1024); tiles of 64 x 64 19 (up to 256), 49 (1024), 180 (4096);
-// of 128 x 128 36 (up to 256), 66 (512), 128 (1024).
 constexpr int64_t kSplitGroups = 512;    // workgroups that a split of k aims at
 
 enum Way { kRows16, kRows32, kTiles64, kTiles128 };
@@ -584,26 +579,46 @@ int64_t tiles(int64_t m, int64_t n, int64_t tm, int64_t tn) {
   return (m + tm - 1) / tm * ((n + tn - 1) / tn);
 }
 
-Way way_of(int64_t m, int64_t n) {
-  if (m <= 16 || tiles(m, n, 16, 16) <= 256) return kRows16;
-  if (m <= 64 || tiles(m, n, 32, 16) <= 512) return kRows32;
-  // a block of k on the busiest CU, in us: 0.18 + 0.35 for each tile of 64 x 64,
-  // 0.1 + 1.0 for each of 128 x 128
-  const double t64 = 0.18 + 0.35 * (double)((tiles(m, n, 64, 64) + 255) / 256);
-  const double t128 = 0.1 + (double)((tiles(m, n, 128, 128) + 255) / 256);
-  return t64 < t128 ? kTiles64 : kTiles128;
-}
+int64_t blocks_of(int64_t k) { return (k + kF8Block - 1) / kF8Block; }
 
 // Parts of k where tiles of 64 x 64 leave CUs idle: of 4 blocks at least.
+int64_t parts_of(int64_t tiles64, int64_t kb) {
+  return std::max<int64_t>(1, std::min(kSplitGroups / tiles64, kb / 4));
+}
+
+// The kernel that takes least, by estimates in us that lie within some 20 % of
+// what was measured (m from 8 to 8192, n from 1000 to 14336, k 1024 and 4096).
+// A few of the measurements, 16 rows at a time, 32, tiles of 64 and of 128, with
+// k = 4096:  32 x 1000 6.8, 8.3, 10.6, 29;   64 x 4096 18.8, 15.0, 13.9, 30;
+// 17 x 14336 25, 20.3, 16.5, 30;   64 x 14336 53, 42, 17.7, 31;   515 x 6144 -, -,
+// 45, 38;   515 x 14336 -, -, 87, 96;   2048 x 6144 -, -, 123, 103.
+Way way_of(int64_t m, int64_t n, int64_t k) {
+  const double kb = (double)blocks_of(k);
+  auto more = [](int64_t x) { return (double)std::max<int64_t>(x, 0); };
+  auto turns = [](int64_t x) { return (double)((x + 255) / 256); };   // on the busiest CU
+  // few rows: a wave's share of k, and the workgroups beyond those that run at once
+  const double t16 = 3.0 + kb * (0.09 + 4.3e-4 * more(tiles(m, n, 16, 16) - 100));
+  const double t32 = 3.3 + kb * (0.13 + 7.0e-4 * more(tiles(m, n, 32, 16) - 250));
+  // tiles: blocks of k one after another, and joining the parts of k
+  const int64_t n64 = tiles(m, n, 64, 64), parts = parts_of(n64, (int64_t)kb);
+  const double t64 = 4.0 + kb / (double)parts * (0.15 + 0.33 * turns(n64 * parts)) +
+                     (parts > 1 ? 1.5 + 0.75 * (double)parts : 0.0);
+  const double t128 = 4.0 + kb * (0.1 + turns(tiles(m, n, 128, 128)));
+  const double tiled = std::min(t64, t128);
+  // the few rows' kernels have the rows in the grid's second dimension
+  if (m <= 65536 && std::min(t16, t32) <= tiled)
+    return m <= 16 || t16 <= t32 ? kRows16 : kRows32;
+  return t64 <= t128 ? kTiles64 : kTiles128;
+}
+
 int64_t splits_of(int64_t m, int64_t n, int64_t k) {
-  if (way_of(m, n) != kTiles64) return 1;
-  const int64_t kb = (k + kF8Block - 1) / kF8Block, t = tiles(m, n, 64, 64);
-  return std::max<int64_t>(1, std::min(kSplitGroups / t, kb / 4));
+  if (m == 0 || n == 0 || way_of(m, n, k) != kTiles64) return 1;
+  return parts_of(tiles(m, n, 64, 64), blocks_of(k));
 }
 
 template <typename T>
 void matmul(const MatmulArgs& a, hipStream_t stream) {
-  switch (way_of(a.m, a.n)) {
+  switch (way_of(a.m, a.n, a.k)) {
     case kRows16: return few<T, 1>(a, stream);
     case kRows32: return few<T, 2>(a, stream);
     case kTiles64: return tiled<T, 1, 1, 1>(a, stream);
@@ -641,7 +656,8 @@ size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d) {
 }
 
 int64_t f8_matmul_groups(const ifq_f8_matmul_desc& d) {
-  switch (way_of(d.m, d.n)) {
+  if (d.m == 0 || d.n == 0) return 0;
+  switch (way_of(d.m, d.n, d.k)) {
     case kRows16: return tiles(d.m, d.n, 16, 16);
     case kRows32: return tiles(d.m, d.n, 32, 16);
     case kTiles64: return tiles(d.m, d.n, 64, 64) * splits_of(d.m, d.n, d.k);

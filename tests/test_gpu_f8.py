@@ -170,6 +170,34 @@ def test_product_tiles_many_and_few(m, n, k, kind, more, rng):
     check_product(rng, m, n, k, kind, **more)
 
 
+@pytest.mark.parametrize("m,n,k,kind,more,split", [
+    (200, 2000, 2064, "bf16", {}, True), (300, 1500, 1296, "f32", dict(ld_a=1312, ld_y=1501), True),
+    (67, 4097, 4096, "f16", dict(ld_w=4112, offset=3), True), (33, 14336, 1040, "bf16", {}, True),
+    (1000, 1500, 400, "bf16", {}, False), (700, 2100, 144, "f32", dict(ld_y=2103), False),
+    (65, 14000, 272, "f16", dict(ld_a=288, ld_w=304, offset=1), False)])
+def test_product_tiles_of_64(m, n, k, kind, more, split, rng):
+    """With k in parts and whole; rows, columns and k that end inside a tile."""
+    d = P.f8_matmul_desc(m, n, k, TYPES[kind][1])
+    assert (P.ifq_f8_matmul_workspace_bytes(d) > 0) == split
+    check_product(rng, m, n, k, kind, **more)
+
+
+@pytest.mark.parametrize("m,n,k", [(200, 2000, 2064), (40, 14000, 2064)])
+def test_product_parts_same_bits_every_time(m, n, k, rng):
+    """One workspace for calls of two sizes, as one program keeps it."""
+    one = P.f8_matmul_desc(m, n, k, P.IFQ_TYPE_F32)
+    two = P.f8_matmul_desc(m + 9, n - 70, k, P.IFQ_TYPE_F32)
+    need = max(P.ifq_f8_matmul_workspace_bytes(d) for d in (one, two))
+    ws = torch.zeros(need, dtype=torch.uint8, device=DEV)
+    outs = []
+    for d in (one, two) * 3:
+        a, sa, w, sw = dev(*operands(np.random.default_rng(d.m), d.m, d.n, k))
+        y = torch.empty(d.m, d.n, device=DEV)
+        P.ifq_f8_matmul(d, a, sa, w, sw, y, ws=ws)
+        outs.append(y)
+    assert need and all(torch.equal(outs[i % 2], y) for i, y in enumerate(outs))
+
+
 @pytest.mark.parametrize("m", [1, 7, 40, 150])
 def test_product_strides(m, rng):
     check_product(rng, m, 77, 272, "bf16", ld_a=304, ld_w=288, ld_y=81)
