@@ -476,50 +476,87 @@ struct Result {
 
 // Joins the parts of a unit's rows in the workgroup that counts itself last.
 // Called by all of a workgroup's threads after they have written its part
-// ([rows][D + 4]: sums, then m and l). Threads that rows and dims leave over
-// take a share of the parts each, eight of them in flight; the order of all
-// additions is the same in every call.
+// ([rows][D + 4]: sums, then m and l). A thread takes four sums of a row at a
+// time, and has 8 or 16 parts' loads in flight: eight parts where there are
+// threads to spare, which then take a share of the parts each, else four parts
+// of four rows (of 128 rows of 128 dims in two parts each in turn took 12 us).
+// The order of all additions is the same in every call.
 template <typename T, int D, int ROWS>
 __device__ __forceinline__ void join_parts(const AttnArgs& a, const Seq& s, int unit, int hk,
                                            int row0, int live, int parts) {
-  constexpr int LD = D + 4, AHEAD = 8;
+  constexpr int LD = D + 4, AHEAD = 8, ITEMS = 4, EACH = 4;
   __shared__ int last;
   __shared__ Result share[256];
   if (!comes_last(a.count + unit, parts, &last)) return;
   const float* src = a.part + (int64_t)unit * a.splits * ROWS * LD;
-  const int items = live * (D / 4), shares = max(1, 256 / items);
-  for (int i0 = 0; i0 < items; i0 += 256) {
-    const int i = i0 + (int)threadIdx.x % (items < 256 ? items : 256);
-    const int mine = items < 256 ? (int)threadIdx.x / items : 0;
-    const bool on = i < items && mine < shares;
-    const int r = on ? i / (D / 4) : 0, d = on ? i % (D / 4) * 4 : 0;
-    Result all = {-__builtin_inff(), 0.0f, {0, 0, 0, 0}};
-    for (int p0 = on ? mine : parts; p0 < parts; p0 += AHEAD * shares) {
-      f32x2 ml[AHEAD], x[AHEAD], y[AHEAD];
+  const int items = live * (D / 4);
+  const Result none = {-__builtin_inff(), 0.0f, {0, 0, 0, 0}};
+  auto store = [&](int r, int d, const Result& all) {
+    store4(out_row<T, D>(a, s, hk, row0 + r) + d, all.o * (all.l == 0.0f ? 0.0f : 1.0f / all.l));
+  };
+  if (items > 256) {
+    for (int i0 = threadIdx.x; i0 < items; i0 += 256 * ITEMS) {
+      Result all[ITEMS];
+      int at[ITEMS], dim[ITEMS];
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const float* at = src + (int64_t)(min(p0 + k * shares, parts - 1) * ROWS + r) * LD;
-        ml[k] = get_pair(at + D);
-        x[k] = get_pair(at + d);
-        y[k] = get_pair(at + d + 2);
+      for (int u = 0; u < ITEMS; ++u) {
+        const int i = min(i0 + 256 * u, items - 1);
+        at[u] = i / (D / 4) * LD;
+        dim[u] = i % (D / 4) * 4;
+        all[u] = none;
+      }
+      for (int p0 = 0; p0 < parts; p0 += EACH) {
+        f32x2 ml[ITEMS][EACH], x[ITEMS][EACH], y[ITEMS][EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+#pragma unroll
+          for (int u = 0; u < ITEMS; ++u) {
+            const float* row = src + (int64_t)min(p0 + k, parts - 1) * ROWS * LD + at[u];
+            ml[u][k] = get_pair(row + D);
+            x[u][k] = get_pair(row + dim[u]);
+            y[u][k] = get_pair(row + dim[u] + 2);
+          }
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+          if (p0 + k < parts)
+#pragma unroll
+            for (int u = 0; u < ITEMS; ++u)
+              all[u].add(ml[u][k][0], ml[u][k][1],
+                         f32x4{x[u][k][0], x[u][k][1], y[u][k][0], y[u][k][1]});
       }
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k)
-        if (p0 + k * shares < parts)
-          all.add(ml[k][0], ml[k][1], f32x4{x[k][0], x[k][1], y[k][0], y[k][1]});
+      for (int u = 0; u < ITEMS; ++u)
+        if (i0 + 256 * u < items) store(at[u] / LD, dim[u], all[u]);
     }
-    if (shares > 1) {
-      share[threadIdx.x] = all;
-      __syncthreads();
-      if (mine == 0)
-        for (int k = 1; k < shares; ++k) {
-          const Result& more = share[threadIdx.x + k * items];
-          all.add(more.m, more.l, more.o);
-        }
+    return;
+  }
+  const int shares = 256 / items;
+  const int i = (int)threadIdx.x % items, mine = (int)threadIdx.x / items;
+  const bool on = mine < shares;
+  const int r = i / (D / 4), d = i % (D / 4) * 4;
+  Result all = none;
+  for (int p0 = on ? mine : parts; p0 < parts; p0 += AHEAD * shares) {
+    f32x2 ml[AHEAD], x[AHEAD], y[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float* row = src + (int64_t)(min(p0 + k * shares, parts - 1) * ROWS + r) * LD;
+      ml[k] = get_pair(row + D);
+      x[k] = get_pair(row + d);
+      y[k] = get_pair(row + d + 2);
     }
-    if (on && mine == 0)
-      store4(out_row<T, D>(a, s, hk, row0 + r) + d,
-             all.o * (all.l == 0.0f ? 0.0f : 1.0f / all.l));
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (p0 + k * shares < parts)
+        all.add(ml[k][0], ml[k][1], f32x4{x[k][0], x[k][1], y[k][0], y[k][1]});
+  }
+  share[threadIdx.x] = all;
+  __syncthreads();
+  if (mine == 0) {
+    for (int k = 1; k < shares; ++k) {
+      const Result& more = share[threadIdx.x + k * items];
+      all.add(more.m, more.l, more.o);
+    }
+    store(r, d, all);
   }
 }
 
@@ -865,20 +902,37 @@ Plan plan_of(const ifq_kv_desc& d) {
   }
   const int64_t at_once = p.few ? p.few : d.head_dim == 64 ? 4 : 2;
   const int64_t steps = (blocks + at_once - 1) / at_once;
-  // With units * steps of work in parts of c steps over kSlots places, the parts'
-  // own cost (kPartSteps steps' time each) and the last part's length add up to
-  // units * steps * kPartSteps / (c * kSlots) + c, least at the root.
-  const double c = std::sqrt((double)p.units * (double)steps * kPartSteps / kSlots);
-  int64_t parts = std::max<int64_t>(1, (int64_t)((double)steps / c + 0.5));
-  // Few rows: at least a workgroup on each CU, as long as its waves have 128 x 128
-  // values each, since parts beside one another cost little more than one (16
-  // sequences of 1000 to 2100 tokens, 128 units: 16.6 us whole, 14.4 in two; one
-  // of 8000, 8 units: 11.8 in 8, 10.4 in 16; but one of 5000 with 64 dims 8.7 in
-  // 10, 9.6 in 20). From 32 on joining them takes what they save (8 units of 64000
-  // tokens: 21.8 us in 32, 24.1 in 64).
+  int64_t parts = 1;
   if (p.few) {
+    // With units * steps of work in parts of c steps over kSlots places, the
+    // parts' own cost (kPartSteps steps' time each) and the last part's length add
+    // up to units * steps * kPartSteps / (c * kSlots) + c, least at the root.
+    const double c = std::sqrt((double)p.units * (double)steps * kPartSteps / kSlots);
+    // At least a workgroup on each CU, as long as its waves have 128 x 128 values
+    // each, since parts beside one another cost little more than one (16 sequences
+    // of 1000 to 2100 tokens, 128 units: 16.6 us whole, 14.4 in two; one of 8000, 8
+    // units: 11.8 in 8, 10.4 in 16; but one of 5000 with 64 dims 8.7 in 10, 9.6 in
+    // 20). From 32 on joining them takes what they save (8 units of 64000 tokens:
+    // 21.8 us in 32, 24.1 in 64).
     const int64_t worth = (steps * p.few * d.head_dim / 512 + 3) / 4;
-    parts = std::max(parts, std::min<int64_t>({(int64_t)kSlots / 2 / p.units, worth, 32}));
+    parts = std::max<int64_t>({1, (int64_t)((double)steps / c + 0.5),
+                               std::min<int64_t>({(int64_t)kSlots / 2 / p.units, worth, 32})});
+  } else {
+    // us, as measured: a step of a workgroup alone on its CU or beside another that
+    // has less to do, and joining parts of 128 rows of 128 dims. 300 queries of 20
+    // heads of 64 over 4000 tokens: 128 us whole, 57 in 3, 42 in 8; 1000 over 2000, 8
+    // heads of 64, 3 sequences: 68 whole, 48 in 3; 500 of 32 heads of 128 over 500:
+    // 25 whole, 33 in two.
+    const double step = d.head_dim == 64 ? 3.8 : d.head_dim == 128 ? 2.25 : 2.8;
+    const double join = (double)std::min<int64_t>(rows, p.rows) * d.head_dim / (128 * 128);
+    double least = 0.0;
+    for (int64_t n = 1; n <= std::min<int64_t>(steps, 32); ++n) {
+      const double groups = (double)(p.units * n) / 256;     // of a CU
+      const double turns = groups <= 1 ? 1.0 : 0.75 * std::max(groups, 2.0);
+      const double time = (double)((steps + n - 1) / n) * step * turns +
+                          (n > 1 ? join * (11.0 + 2.0 * (double)n) : 0.0);
+      if (n == 1 || time < least) least = time, parts = n;
+    }
   }
   int64_t chunk = (steps + parts - 1) / parts;
   if (p.few) chunk = (chunk + 3) / 4 * 4;      // the four waves take a step each
