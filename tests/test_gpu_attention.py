@@ -159,6 +159,24 @@ def test_long_sequences_split(max_kv, rng):
     Case(rng, [2, 1], [1033, 3000], 4, 1, 128, 64, "bf16", max_kv=max_kv, spread=6.0).check()
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,max_kv", [
+    ([19], [1400], 4, 2, 1400),              # few rows of a block used, many parts
+    ([150], [900], 3, 1, 5000),              # planned for longer: parts that do not exist
+    ([70, 9, 0], [800, 33, 7], 4, 1, 800), ([60], [2000], 5, 1, 70)])
+def test_many_tokens_split(dim, new, lens, heads, kv_heads, max_kv, rng):
+    """Many query rows over long sequences: parts joined, the same bits each time."""
+    c = Case(rng, new, lens, heads, kv_heads, dim, 64, "f16" if dim == 128 else "bf16",
+             max_kv=max_kv)
+    need = P.ifq_kv_attention_workspace_bytes(c.desc)
+    assert max_kv < 100 or need > 0
+    ws = torch.zeros(max(need, 1), dtype=torch.uint8, device=DEV)
+    c.check(ws=ws)
+    outs = [c.run(ws=ws), c.run(), c.run(ws=ws)]
+    assert all(torch.equal(outs[0], o) for o in outs[1:])
+    assert not ws[:65536].any()
+
+
 def test_sharp_and_flat_scores(rng):
     Case(rng, [1, 9], [600, 300], 8, 2, 128, 32, "f16", spread=20.0).check()
     Case(rng, [1, 9], [600, 300], 8, 2, 128, 32, "f16", spread=0.0).check()
