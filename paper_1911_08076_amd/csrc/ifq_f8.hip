@@ -25,21 +25,16 @@ struct QuantArgs {
 constexpr float kMinTop = 0x1p-96f;
 constexpr uint32_t kInfBits = 0x7F800000u;
 
-// Eight consecutive values of a row, as fp32; zeros from k on.
-template <typename T, bool VEC>
+// Eight consecutive values of a row, as fp32; zeros from k on. Rows may begin at
+// any element: the copies become loads of 16 bytes whatever the address (rows of
+// 4095 bfloat16 element by element, 8192 of them: 47 us instead of 21).
+template <typename T>
 __device__ __forceinline__ void load8(const T* row, int c, int k, float* v) {
-  if (VEC && c + 8 <= k) {
-    if constexpr (sizeof(T) == 4) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(row + c);
-      const f32x4 b = *reinterpret_cast<const f32x4*>(row + c + 4);
+  if (c + 8 <= k) {
+    T x[8];
+    __builtin_memcpy(x, row + c, sizeof(x));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-    } else {
-      typedef T t8 __attribute__((ext_vector_type(8)));
-      const t8 a = *reinterpret_cast<const t8*>(row + c);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
-    }
+    for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
     return;
   }
 #pragma unroll
@@ -94,7 +89,7 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
 // Bound by memory: 8192 x 14336 bfloat16 values 73 us, 4.9 TB/s (a copy of 4 GiB
 // reaches 4.64), with vector instructions on 81 % of the cycles; one row of 4096
 // takes 2.0 us on the GPU, the latency of a launch.
-template <typename T, bool VEC, int ROWS>
+template <typename T, int ROWS>
 __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
   constexpr int PER = ROWS == 16 ? 4 : 1;
   const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
@@ -107,7 +102,7 @@ __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
   const int k16 = (a.k + 15) & ~15;
   float v[PER][8];
 #pragma unroll
-  for (int p = 0; p < PER; ++p) load8<T, VEC>(src, (b0 + p) * kF8Block + 8 * l, a.k, v[p]);
+  for (int p = 0; p < PER; ++p) load8(src, (b0 + p) * kF8Block + 8 * l, a.k, v[p]);
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int b = b0 + p, c = b * kF8Block + 8 * l;
@@ -120,7 +115,7 @@ __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
 
 // A scale per 128 x 128: a workgroup holds the block in registers, 64 values to
 // a thread, so that it too is read once. For weights, when they are loaded.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   __shared__ uint32_t part[4];
   const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
@@ -133,7 +128,7 @@ __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   for (int i = 0; i < 8; ++i) {
     const int row = by * kF8Block + 16 * i + g;
     if (row < a.rows) {
-      load8<T, VEC>(static_cast<const T*>(a.x) + (int64_t)row * a.ld_x, c, a.k, v[i]);
+      load8(static_cast<const T*>(a.x) + (int64_t)row * a.ld_x, c, a.k, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
@@ -157,7 +152,7 @@ __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   if (threadIdx.x == 0) a.scales[(int64_t)bx * a.rb + by] = scale_of(top);
 }
 
-template <typename T, bool VEC>
+template <typename T>
 hipError_t quantize(QuantArgs a, int block_rows, hipStream_t stream) {
   // Row by row where three quarters of its workgroups have work, or where rows
   // are few (us, row by row and 16 rows at a time: 16 x 4096 2.8 and 4.4, 1024 x
@@ -171,19 +166,12 @@ hipError_t quantize(QuantArgs a, int block_rows, hipStream_t stream) {
   if (a.wide * high > kMaxGroups) return hipErrorInvalidConfiguration;
   const dim3 grid((uint32_t)(a.wide * high)), block(256);
   if (block_rows == 128)
-    hipLaunchKernelGGL((f8_quantize_blocks<T, VEC>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((f8_quantize_blocks<T>), grid, block, 0, stream, a);
   else if (one)
-    hipLaunchKernelGGL((f8_quantize_rows<T, VEC, 1>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((f8_quantize_rows<T, 1>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((f8_quantize_rows<T, VEC, 16>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((f8_quantize_rows<T, 16>), grid, block, 0, stream, a);
   return hipGetLastError();
-}
-
-template <typename T>
-hipError_t quantize(const QuantArgs& a, int block_rows, hipStream_t stream) {
-  const bool vec = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ld_x * sizeof(T) % 16 == 0;
-  return vec ? quantize<T, true>(a, block_rows, stream)
-             : quantize<T, false>(a, block_rows, stream);
 }
 
 // --- product --------------------------------------------------------------------
@@ -221,23 +209,19 @@ __device__ __forceinline__ f16x8 halves(uint32_t a, uint32_t b) {
   return f16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
+// Four sums of a row of y, or what is left of it; a row may begin at any element.
 template <typename T>
-__device__ __forceinline__ void store4(T* p, f32x4 v, bool vec, int left) {
+__device__ __forceinline__ void store4(T* p, f32x4 v, int left) {
   typedef T t4 __attribute__((ext_vector_type(4)));
+  typedef t4 any4 __attribute__((aligned(sizeof(T))));
   const t4 r = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-  if (vec && left >= 4) {
-    *reinterpret_cast<t4*>(p) = r;
+  if (left >= 4) {
+    *reinterpret_cast<any4*>(p) = r;
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < left) p[i] = r[i];
   }
-}
-
-// Whether rows of y can be written four elements at a time.
-template <typename T>
-__device__ __forceinline__ bool vectors(const MatmulArgs& a) {
-  return reinterpret_cast<uintptr_t>(a.y) % (4 * sizeof(T)) == 0 && a.ld_y % 4 == 0;
 }
 
 // Few activation rows: the weights are read once, and only the latency and
@@ -313,14 +297,13 @@ __global__ __launch_bounds__(64 * KS) void f8_matmul_few(MatmulArgs a) {
 #pragma unroll
   for (int x = 0; x < MT; ++x) *reinterpret_cast<f32x4*>(sums[wave][x][lane]) = acc[x];
   __syncthreads();
-  const bool vec = vectors<T>(a);
   for (int i = threadIdx.x; i < 64 * MT; i += 64 * KS) {
     const int x = i >> 6, l = i & 63, n = n0 + 4 * (l >> 4), mm = m0 + 16 * x + (l & 15);
     f32x4 v = *reinterpret_cast<const f32x4*>(sums[0][x][l]);
 #pragma unroll
     for (int w = 1; w < KS; ++w) v += *reinterpret_cast<const f32x4*>(sums[w][x][l]);
     if (mm < a.m && n < a.n)
-      store4(static_cast<T*>(a.y) + (int64_t)mm * a.ld_y + n, v, vec, a.n - n);
+      store4(static_cast<T*>(a.y) + (int64_t)mm * a.ld_y + n, v, a.n - n);
   }
 }
 
@@ -534,7 +517,6 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void f8_matmul_tiled(MatmulAr
         acc[0][0][e + 1] += v[1];
       }
   }
-  const bool vec = vectors<T>(a);
 #pragma unroll
   for (int x = 0; x < MT; ++x) {
     const int mm = m0 + wm + 32 * x + r;
@@ -547,7 +529,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void f8_matmul_tiled(MatmulAr
         const int n = n0 + wn + 32 * z + 8 * e + 4 * h;
         if (n < a.n)
           store4(y + n, f32x4{acc[x][z][4 * e], acc[x][z][4 * e + 1], acc[x][z][4 * e + 2],
-                              acc[x][z][4 * e + 3]}, vec, a.n - n);
+                              acc[x][z][4 * e + 3]}, a.n - n);
       }
   }
 }
