@@ -72,12 +72,12 @@ struct WinGeom {
   FastDiv div_u, div_win, div_rimg, div_nks, div_kw;
 };
 
-// One LDS-DMA load of 4 bytes per lane (16 in dma16).
+// One LDS-DMA load of 4 bytes per lane (16 in dma16); the s_nop as there.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma4(const void* src, uint32_t dst) {
   const uint32_t d = __builtin_amdgcn_readfirstlane(dst);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :: "s"(d), "v"(src) : "memory", "m0");
 }
 #pragma clang diagnostic pop

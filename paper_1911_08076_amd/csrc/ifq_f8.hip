@@ -312,15 +312,16 @@ __device__ const u32x4 g_zero16 = {0, 0, 0, 0};
 
 // 16 bytes per lane straight into LDS at dst (uniform) + 16 * lane: from a
 // pointer per lane, or from a uniform base and an offset per lane. The waits
-// for them are the caller's.
+// for them are the caller's. A load into LDS must not follow the write of M0
+// directly: one wait state, which the compiler does not add inside asm.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds16(const void* src, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :: "s"(dst), "v"(src) : "memory", "m0");
 }
 __device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t off, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(dst), "v"(off), "s"(base) : "memory", "m0");
 }
 #pragma clang diagnostic pop

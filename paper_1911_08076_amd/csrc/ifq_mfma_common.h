@@ -28,13 +28,15 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
 }
 
 // One wave-wide LDS-DMA load: 16 bytes per lane from src to LDS dst + 16*lane.
-// M0 carries the LDS base; nothing else in these kernels uses M0.
+// M0 carries the LDS base; nothing else in these kernels uses M0. A load into
+// LDS needs a wait state after the write of M0, which the compiler does not add
+// inside asm: the s_nop.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 // dst must be wave-uniform (it is moved to SGPRs explicitly).
 __device__ __forceinline__ void dma16(const void* src, uint32_t dst) {
   const uint32_t d = __builtin_amdgcn_readfirstlane(dst);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :: "s"(d), "v"(src) : "memory", "m0");
 }
 
@@ -48,7 +50,7 @@ __device__ __forceinline__ void dma16s(const void* base, uint32_t voff, uint32_t
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
   const uint64_t bs = ((uint64_t)hi << 32) | (uint64_t)lo;
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(d), "v"(voff), "s"(bs) : "memory", "m0");
 }
 #pragma clang diagnostic pop
