@@ -124,7 +124,10 @@ __device__ __forceinline__ float sum_g(float x) {
 }
 
 // What the query rows of a wave see: blocks of 32 positions, first those of
-// the sinks, then those from the window's begin to the last position.
+// the sinks, then those from the window's begin to the last position. p_lo and
+// p_hi are the positions of the first and the last query, end the last position
+// held: a sequence may be longer than its page table, and then the window may
+// begin past it.
 struct View {
   int32_t blocks, sink_blocks, first;   // first: block where the window begins
   __device__ __forceinline__ int block(int i) const {
@@ -132,14 +135,15 @@ struct View {
   }
 };
 
-__device__ __forceinline__ View view_of(const AttnArgs& a, int p_lo, int p_hi) {
+__device__ __forceinline__ View view_of(const AttnArgs& a, int p_lo, int p_hi, int end) {
   View v = {0, 0, 0};
-  if (p_hi < 0) return v;
+  if (min(p_hi, end) < 0) return v;
+  const int held = min(p_hi, end) / kCodeTokens + 1;       // blocks
   const int lo = a.window > 0 ? max(p_lo - a.window + 1, 0) : 0;
   v.first = lo / kCodeTokens;
   if (a.window > 0)
-    v.sink_blocks = min((a.sinks + kCodeTokens - 1) / kCodeTokens, v.first);
-  v.blocks = v.sink_blocks + p_hi / kCodeTokens - v.first + 1;
+    v.sink_blocks = min((a.sinks + kCodeTokens - 1) / kCodeTokens, min(v.first, held));
+  v.blocks = v.sink_blocks + max(held - v.first, 0);
   return v;
 }
 
@@ -232,9 +236,9 @@ struct State {
   }
 };
 
-// Whether the query at position pos sees position j.
-__device__ __forceinline__ bool sees(const AttnArgs& a, int pos, int j) {
-  return j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
+// Whether the query at position pos sees position j; end: the last position held.
+__device__ __forceinline__ bool sees(const AttnArgs& a, int pos, int end, int j) {
+  return j <= min(pos, end) && (a.window == 0 || j > pos - a.window || j < a.sinks);
 }
 
 // A block's place: its page's head (page 0 where the cache has no such page,
@@ -297,13 +301,13 @@ __device__ __forceinline__ Place pick(const Place (&p)[N], int k) {
 // columns, U blocks (U * i ..) at a step: column n stands for query row
 // n % (16 / U) and sees only block n / (16 / U) of the U, so that with few
 // rows all columns take part in the softmax. pos: the position of this lane's
-// query. A step's loads are issued a step ahead: the keys' after their last
-// use, the values' likewise.
+// query; p_lo, p_hi and last_held: as for view_of. A step's loads are issued a step
+// ahead: the keys' after their last use, the values' likewise.
 template <typename T, int D, int U>
 __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int b, int hk,
                                        int begin, int end, int step,
                                        const typename Half<T>::x8 (&q)[D / 32], int pos,
-                                       int p_lo, int p_hi, State<D>& s) {
+                                       int p_lo, int p_hi, int last_held, State<D>& s) {
   typedef Half<T> H;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int mine = n / (16 / U);          // the block of the U that this column sees
@@ -363,7 +367,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
     bool masked = false;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      masked |= !now[u].held || now[u].j0 + kCodeTokens - 1 > p_lo ||
+      masked |= !now[u].held || now[u].j0 + kCodeTokens - 1 > min(p_lo, last_held) ||
                 (a.window > 0 && now[u].j0 <= p_hi - a.window);
     float sc[8];
 #pragma unroll
@@ -395,7 +399,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
     if (masked) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool ok = own.held && sees(a, pos, own.j0 + 16 * (e >> 2) + 4 * g + (e & 3));
+        const bool ok =
+            own.held && sees(a, pos, last_held, own.j0 + 16 * (e >> 2) + 4 * g + (e & 3));
         sc[e] = ok ? sc[e] : -__builtin_inff();
         // what a hidden row holds must not reach the sums, not even as 0 * NaN
         vt[e] = ok ? vt[e] : 0.0f;
@@ -427,8 +432,14 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const View& view, int 
   s.ob = sum_g(s.ob);
 }
 
-// Query row `row` of a sequence (row = token * ratio + head of the group) as
-// this lane's operand column, and its position; rows past the last repeat it.
+// Position of query row `row` of a sequence (row = token * ratio + head of the
+// group): where no mask is causal, the last.
+__device__ __forceinline__ int position_of(const AttnArgs& a, const Seq& s, int row) {
+  return a.causal ? s.pos + row / a.ratio : s.length - 1;
+}
+
+// A query row as this lane's operand column, and its position; rows past the
+// last repeat it.
 template <typename T, int D>
 __device__ __forceinline__ void load_row(const AttnArgs& a, const Seq& s, int hk, int row,
                                          typename Half<T>::x8 (&q)[D / 32], int& pos) {
@@ -440,7 +451,7 @@ __device__ __forceinline__ void load_row(const AttnArgs& a, const Seq& s, int hk
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
     q[i] = *reinterpret_cast<const typename Half<T>::x8*>(src + 8 * i);
-  pos = a.causal ? min(s.pos + token, s.length - 1) : s.length - 1;
+  pos = position_of(a, s, row);
 }
 
 template <typename T, int D>
@@ -584,10 +595,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_few(AttnAr
   const int rows = s.count * a.ratio, row0 = rb * ROWS;
   if (row0 >= rows) return;
   const int live = min(ROWS, rows - row0);
-  const int p_lo = a.causal ? min(s.pos + row0 / a.ratio, s.length - 1) : s.length - 1;
-  const int p_hi = a.causal ? min(s.pos + (row0 + live - 1) / a.ratio, s.length - 1)
-                            : s.length - 1;
-  const View view = view_of(a, p_lo, p_hi);
+  const int p_lo = position_of(a, s, row0), p_hi = position_of(a, s, row0 + live - 1);
+  const View view = view_of(a, p_lo, p_hi, s.length - 1);
   // parts of `chunk` steps; longer ones where the sequence is longer than planned
   const int steps = (view.blocks + U - 1) / U;
   const int chunk = max(a.chunk, (steps + a.splits - 1) / a.splits);
@@ -598,7 +607,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_few(AttnAr
   load_row<T, D>(a, s, hk, row0 + n % ROWS, q, pos);
   State<D> st;
   attend<T, D, U>(a, view, b, hk, part * chunk + wave, min(steps, (part + 1) * chunk), 4, q, pos,
-                  p_lo, p_hi, st);
+                  p_lo, p_hi, s.length - 1, st);
   const float corr = st.ob - 24.0f * st.wsum[0];
 #pragma unroll
   for (int d = 0; d < D / 16; ++d)
@@ -675,11 +684,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
   const Seq s = seq_of(c, b);
   const int rows = s.count * a.ratio;
   if (rb * ROWS >= rows) return;
-  auto position = [&](int row) {
-    return a.causal ? min(s.pos + row / a.ratio, s.length - 1) : s.length - 1;
-  };
+  const int last_held = s.length - 1;
   const int live = min(ROWS, rows - rb * ROWS);
-  const View view = view_of(a, position(rb * ROWS), position(rb * ROWS + live - 1));
+  const View view = view_of(a, position_of(a, s, rb * ROWS),
+                            position_of(a, s, rb * ROWS + live - 1), last_held);
   const int steps = (view.blocks + NB - 1) / NB;
   const int chunk = max(a.chunk, (steps + a.splits - 1) / a.splits);
   const int parts = max(1, (steps + chunk - 1) / chunk);
@@ -687,8 +695,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
   const int begin = part * chunk, end = min(steps, begin + chunk);
   const int row0 = rb * ROWS + wave * WROWS;
   const int own = min(WROWS, rows - row0);         // may be below 1: the wave only helps
-  const int p_lo = own > 0 ? position(row0) : 0;
-  const int p_hi = own > 0 ? position(row0 + own - 1) : -1;
+  const int p_lo = own > 0 ? position_of(a, s, row0) : 0;
+  const int p_hi = own > 0 ? position_of(a, s, row0 + own - 1) : -1;
 
   typename H::x8 q[TILES][D / 32];
   int pos[TILES];
@@ -787,10 +795,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
       for (int k = 0; k < NB; ++k) {
         const int j0 = now[k].j0;
         // blocks that none of the wave's rows sees
-        if (!now[k].held || j0 > p_hi ||
+        if (!now[k].held || j0 > min(p_hi, last_held) ||
             (a.window > 0 && j0 + kCodeTokens - 1 <= p_lo - a.window && j0 >= a.sinks))
           continue;
-        const bool masked = j0 + kCodeTokens - 1 > p_lo ||
+        const bool masked = j0 + kCodeTokens - 1 > min(p_lo, last_held) ||
                             (a.window > 0 && j0 <= p_hi - a.window);
         float sc[TILES][8];
 #pragma unroll
@@ -820,7 +828,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
           for (int x = 0; x < TILES; ++x)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (!sees(a, pos[x], j0 + 16 * (e >> 2) + 4 * g + (e & 3)))
+              if (!sees(a, pos[x], last_held, j0 + 16 * (e >> 2) + 4 * g + (e & 3)))
                 sc[x][e] = -__builtin_inff();
         }
 #pragma unroll
