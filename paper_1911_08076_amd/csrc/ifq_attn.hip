@@ -44,6 +44,7 @@ struct AttnArgs {
   int64_t q_stride, o_stride;
   int32_t ratio;        // query heads per key/value head
   int32_t causal, window, sinks;
+  int32_t sink_blocks;  // blocks of 32 positions that hold the sinks
   float factor;         // scale * log2(e)
   int32_t row_blocks;   // blocks of a sequence's ratio * max_q query rows
   FastDiv div_page;       // by the blocks of 32 tokens of a page
@@ -139,10 +140,11 @@ __device__ __forceinline__ View view_of(const AttnArgs& a, int p_lo, int p_hi, i
   View v = {0, 0, 0};
   if (min(p_hi, end) < 0) return v;
   const int held = min(p_hi, end) / kCodeTokens + 1;       // blocks
-  const int lo = a.window > 0 ? max(p_lo - a.window + 1, 0) : 0;
+  // queries before position 0 see nothing; without them no difference to a window
+  // overflows, however wide it is
+  const int lo = a.window > 0 ? max(max(p_lo, 0) - a.window + 1, 0) : 0;
   v.first = lo / kCodeTokens;
-  if (a.window > 0)
-    v.sink_blocks = min((a.sinks + kCodeTokens - 1) / kCodeTokens, min(v.first, held));
+  if (a.window > 0) v.sink_blocks = min(a.sink_blocks, min(v.first, held));
   v.blocks = v.sink_blocks + max(held - v.first, 0);
   return v;
 }
@@ -238,7 +240,7 @@ struct State {
 
 // Whether the query at position pos sees position j; end: the last position held.
 __device__ __forceinline__ bool sees(const AttnArgs& a, int pos, int end, int j) {
-  return j <= min(pos, end) && (a.window == 0 || j > pos - a.window || j < a.sinks);
+  return j <= min(pos, end) && (a.window == 0 || j > max(pos, 0) - a.window || j < a.sinks);
 }
 
 // A block's place: its page's head (page 0 where the cache has no such page,
@@ -796,7 +798,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
         const int j0 = now[k].j0;
         // blocks that none of the wave's rows sees
         if (!now[k].held || j0 > min(p_hi, last_held) ||
-            (a.window > 0 && j0 + kCodeTokens - 1 <= p_lo - a.window && j0 >= a.sinks))
+            (a.window > 0 && j0 + kCodeTokens - 1 <= max(p_lo, 0) - a.window && j0 >= a.sinks))
           continue;
         const bool masked = j0 + kCodeTokens - 1 > min(p_lo, last_held) ||
                             (a.window > 0 && j0 <= p_hi - a.window);
@@ -886,6 +888,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
   if (parts > 1) join_parts<T, D, ROWS>(a, s, unit, hk, rb * ROWS, live, parts);
 }
 
+// Blocks of 32 tokens that n tokens fill.
+int64_t code_blocks(int64_t n) { return (n + kCodeTokens - 1) / kCodeTokens; }
+
 // Which kernel, and how its work is split.
 struct Plan {
   int32_t few;            // blocks of a step for few rows (U), 0: many rows
@@ -902,10 +907,10 @@ Plan plan_of(const ifq_kv_desc& d) {
   p.row_blocks = (int32_t)((rows + p.rows - 1) / p.rows);
   p.units = (int64_t)d.batch * d.kv_heads * p.row_blocks;
   // blocks that a unit may see, and steps of them
-  int64_t blocks = ((int64_t)d.max_kv + kCodeTokens - 1) / kCodeTokens + 1;
+  int64_t blocks = code_blocks(d.max_kv) + 1;
   if (d.window > 0) {
     const int64_t seen = ((int64_t)d.window + d.max_q + kCodeTokens) / kCodeTokens +
-                         (d.sinks + kCodeTokens - 1) / kCodeTokens + 1;
+                         code_blocks(d.sinks) + 1;
     blocks = std::min(blocks, seen);
   }
   const int64_t at_once = p.few ? p.few : d.head_dim == 64 ? 4 : 2;
@@ -999,6 +1004,7 @@ hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs
   a.causal = d.causal;
   a.window = d.window;
   a.sinks = d.sinks;
+  a.sink_blocks = (int32_t)code_blocks(d.sinks);
   a.factor = d.scale * 1.4426950408889634f;
   a.row_blocks = p.row_blocks;
   a.div_page = make_fastdiv((uint32_t)(d.page_tokens / kCodeTokens));

@@ -1,11 +1,12 @@
 """Attention at the ends of its arguments' ranges: sequences longer than their page
-table. Against the oracle, as in
+table, windows and sinks up to the largest int32. Against the oracle, as in
 test_gpu_attention."""
 import pytest
 
 from test_gpu_attention import Case
 
 pytestmark = pytest.mark.gpu
+INT_MAX = 2 ** 31 - 1
 
 
 @pytest.mark.parametrize("new", [[1, 1], [3, 2], [60, 9], [300, 200]])
@@ -17,3 +18,14 @@ def test_sequences_longer_than_their_table(new, window, sinks, past, rng):
     c = Case(rng, new, [512, 512], 4, 2, 64, 32, "f16", window=window, sinks=sinks)
     c.lens = [512 + past, 512 + past // 2]
     c.check()
+
+
+@pytest.mark.parametrize("new,lens", [([1, 1], [300, 40]), ([6], [3]), ([40, 7], [20, 5]),
+                                      ([300], [200]), ([300, 9], [310, 90])])
+@pytest.mark.parametrize("window,sinks", [
+    (INT_MAX, 0), (INT_MAX, INT_MAX), (INT_MAX - 1, 4), (INT_MAX - 40, 0), (7, INT_MAX),
+    (7, INT_MAX - 30), (7, INT_MAX - 31), (33, INT_MAX - 1)])
+def test_largest_windows_and_sinks(new, lens, window, sinks, rng):
+    """Sequences shorter than what asks among them: their first queries' positions are
+    negative, and see nothing."""
+    Case(rng, new, lens, 4, 2, 64, 32, "bf16", window=window, sinks=sinks).check()
