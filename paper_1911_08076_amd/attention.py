@@ -46,38 +46,48 @@ class _Workspace:
         return self._all[-1]
 
 
-def _check_rows(x, columns, types):
+def _check_rows(x, columns, types, device):
     if x.dim() != 2 or x.shape[1] != columns or not x.is_contiguous() or x.dtype not in types:
         raise ValueError("dense rows of %d values of %s expected, got %s of %s" % (
             columns, " or ".join(str(t) for t in types), tuple(x.shape), x.dtype))
+    if x.device != device:
+        raise ValueError("rows on %s expected, got them on %s" % (device, x.device))
+
+
+def _check_out(out, x, columns):
+    _check_rows(out, columns, (x.dtype,), x.device)
+    if out.shape[0] != x.shape[0]:
+        raise ValueError("an output of %d rows for %d" % (out.shape[0], x.shape[0]))
 
 
 class F8Linear:
     """Weights [out][in] in 8-bit floats with a scale per 128 x 128, and y = x w^T
     for x quantized with a scale per row and 128 columns. Calls share a workspace,
-    so they follow one another: on one stream, or ordered by events."""
+    so they follow one another: on one stream, or ordered by events. All tensors
+    are on the weights' GPU."""
 
     def __init__(self, weight, workspace=None):
-        _check_rows(weight, weight.shape[-1], tuple(_TYPES))
+        _check_rows(weight, weight.shape[-1], tuple(_TYPES), weight.device)
+        dev = weight.device
+        if dev.type != "cuda":
+            raise ValueError("weights on a GPU expected, got them on %s" % dev)
         n, k = weight.shape
         self.n, self.k, self.ld = n, k, -(-k // 16) * 16
         self.workspace = _Workspace() if workspace is None else workspace
-        dev = weight.device
         self.codes = torch.empty(n, self.ld, dtype=torch.uint8, device=dev)
         self.scales = torch.empty(-(-k // 128), -(-n // 128), device=dev)
-        P.ifq_f8_quantize(P.f8_quant_desc(n, k, _TYPES[weight.dtype], block_rows=128), weight,
-                          self.codes, self.scales)
+        P.ifq_f8_quantize(P.f8_quant_desc(n, k, _TYPES[weight.dtype], block_rows=128),
+                          weight, self.codes, self.scales)
 
     def __call__(self, x, out=None):
         """x [m][k] -> [m][n] of x's type."""
-        _check_rows(x, self.k, tuple(_TYPES))
-        m, dev = x.shape[0], x.device
+        dev = self.codes.device
+        _check_rows(x, self.k, tuple(_TYPES), dev)
+        m = x.shape[0]
         if out is None:
             out = torch.empty(m, self.n, dtype=x.dtype, device=dev)
         else:
-            _check_rows(out, self.n, (x.dtype,))
-            if out.shape[0] != m:
-                raise ValueError("an output of %d rows for %d" % (out.shape[0], m))
+            _check_out(out, x, self.n)
         if m == 0:
             return out
         codes = torch.empty(m, self.ld, dtype=torch.uint8, device=dev)
@@ -94,7 +104,7 @@ class AttentionLayer:
     weight_out [hidden][heads * head_dim]; num_pages pages of page_tokens tokens,
     of which a sequence may have max_pages. rot_dim None: the whole head. Steps
     share the cache and a workspace, so they follow one another: on one stream,
-    or ordered by events."""
+    or ordered by events. All tensors are on the weights' GPU."""
 
     def __init__(self, weight_qkv, weight_out, heads, kv_heads, head_dim, num_pages, max_pages,
                  page_tokens=64, rot_dim=None, rot_base=10000.0, window=0, sinks=0):
@@ -107,6 +117,9 @@ class AttentionLayer:
             raise ValueError("weights of shapes %s and %s do not fit %d and %d heads of %d" % (
                 tuple(weight_qkv.shape), tuple(weight_out.shape), heads, kv_heads, head_dim))
         dev = weight_qkv.device
+        if weight_out.device != dev:
+            raise ValueError("weights on one GPU expected, got them on %s and %s" % (
+                dev, weight_out.device))
         self.workspace = _Workspace()
         self.qkv = F8Linear(weight_qkv, self.workspace)
         self.out = F8Linear(weight_out, self.workspace)
@@ -134,17 +147,20 @@ class AttentionLayer:
         ifq_kv_append; max_q: the most new tokens of a sequence; max_kv: about how
         long the longest sequence is, for the split of the work. Returns
         [tokens][hidden]."""
-        _check_rows(x, self.qkv.k, (torch.bfloat16, torch.float16))
+        dev = self.cache.device
+        _check_rows(x, self.qkv.k, (torch.bfloat16, torch.float16), dev)
         tokens, batch = x.shape[0], lengths.numel()
         for name, t, shape in (("offsets", offsets, (batch + 1,)), ("lengths", lengths, (batch,)),
                                ("pages", pages, (batch, self.max_pages))):
             if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous():
                 raise ValueError("%s: dense int32 of shape %s expected, got %s of %s" % (
                     name, shape, tuple(t.shape), t.dtype))
+            if t.device != dev:
+                raise ValueError("%s: expected on %s, got on %s" % (name, dev, t.device))
         if max_kv is None:
             max_kv = self.max_pages * self.page_tokens
         rows = self.qkv(x)
-        q = torch.empty(tokens, self.heads * self.head_dim, dtype=x.dtype, device=x.device)
+        q = torch.empty(tokens, self.heads * self.head_dim, dtype=x.dtype, device=dev)
         mixed = torch.empty_like(q)
         if tokens:
             k = rows[:, self.heads * self.head_dim:]
@@ -156,5 +172,5 @@ class AttentionLayer:
             d = self._desc(batch, tokens, max_q, max_kv, x.dtype)
             P.ifq_kv_attention(d, q, offsets, lengths, pages, self.cache, mixed,
                                ws=self.workspace.get(P.ifq_kv_attention_workspace_bytes(d),
-                                                     x.device))
+                                                     dev))
         return self.out(mixed, out=out)
