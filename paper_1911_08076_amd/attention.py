@@ -157,6 +157,8 @@ class AttentionLayer:
                     name, shape, tuple(t.shape), t.dtype))
             if t.device != dev:
                 raise ValueError("%s: expected on %s, got on %s" % (name, dev, t.device))
+        if out is not None:
+            _check_out(out, x, self.out.n)
         if max_kv is None:
             max_kv = self.max_pages * self.page_tokens
         rows = self.qkv(x)

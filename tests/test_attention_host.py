@@ -67,7 +67,7 @@ def arguments(dev):
 
 
 @pytest.mark.parametrize("elsewhere", ["cpu", "cuda:1"])
-@pytest.mark.parametrize("name", ["x", "offsets", "lengths", "pages"])
+@pytest.mark.parametrize("name", ["x", "offsets", "lengths", "pages", "out"])
 def test_what_is_not_on_the_layers_gpu_is_refused(launches, name, elsewhere):
     attend = layer()
     launches.seen.clear()
@@ -82,4 +82,15 @@ def test_weights_off_the_gpu_or_on_two_are_refused(launches):
     for dev, dev2 in (("cpu", None), ("cuda:0", "cpu"), ("cuda:0", "cuda:1")):
         with pytest.raises(ValueError):
             layer(dev, dev2)
+    assert launches.seen == []
+
+
+@pytest.mark.parametrize("change", [(3, 63), (2, 64)])
+def test_an_output_that_does_not_fit_is_refused_before_the_append(launches, change):
+    attend = layer()
+    launches.seen.clear()
+    args = arguments("cuda:0")
+    args["out"] = torch.empty(*change, dtype=BF16, device="cuda:0")
+    with pytest.raises(ValueError):
+        attend(**args, max_q=3)
     assert launches.seen == []
