@@ -8,6 +8,8 @@ queries, keys and values, append (with the rotation), attention, quantize,
 product. Nothing in it waits for the GPU or reads the sequences' lengths on the
 host, so a step on fixed inputs can be captured in a graph.
 """
+import contextlib
+
 import torch
 
 from . import _ffi
@@ -60,6 +62,14 @@ def _check_out(out, x, columns):
         raise ValueError("an output of %d rows for %d" % (out.shape[0], x.shape[0]))
 
 
+def _on(device):
+    """The launches and temporaries of a layer go to its own GPU's current stream,
+    also where another GPU is torch's current one."""
+    if device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
 class F8Linear:
     """Weights [out][in] in 8-bit floats with a scale per 128 x 128, and y = x w^T
     for x quantized with a scale per row and 128 columns. Calls share a workspace,
@@ -76,8 +86,9 @@ class F8Linear:
         self.workspace = _Workspace() if workspace is None else workspace
         self.codes = torch.empty(n, self.ld, dtype=torch.uint8, device=dev)
         self.scales = torch.empty(-(-k // 128), -(-n // 128), device=dev)
-        P.ifq_f8_quantize(P.f8_quant_desc(n, k, _TYPES[weight.dtype], block_rows=128),
-                          weight, self.codes, self.scales)
+        with _on(dev):
+            P.ifq_f8_quantize(P.f8_quant_desc(n, k, _TYPES[weight.dtype], block_rows=128),
+                              weight, self.codes, self.scales)
 
     def __call__(self, x, out=None):
         """x [m][k] -> [m][n] of x's type."""
@@ -90,12 +101,13 @@ class F8Linear:
             _check_out(out, x, self.n)
         if m == 0:
             return out
-        codes = torch.empty(m, self.ld, dtype=torch.uint8, device=dev)
-        scales = torch.empty(self.scales.shape[0], m, device=dev)
-        P.ifq_f8_quantize(P.f8_quant_desc(m, self.k, _TYPES[x.dtype]), x, codes, scales)
-        mm = P.f8_matmul_desc(m, self.n, self.ld, _TYPES[x.dtype])
-        P.ifq_f8_matmul(mm, codes, scales, self.codes, self.scales, out,
-                        ws=self.workspace.get(P.ifq_f8_matmul_workspace_bytes(mm), dev))
+        with _on(dev):
+            codes = torch.empty(m, self.ld, dtype=torch.uint8, device=dev)
+            scales = torch.empty(self.scales.shape[0], m, device=dev)
+            P.ifq_f8_quantize(P.f8_quant_desc(m, self.k, _TYPES[x.dtype]), x, codes, scales)
+            mm = P.f8_matmul_desc(m, self.n, self.ld, _TYPES[x.dtype])
+            P.ifq_f8_matmul(mm, codes, scales, self.codes, self.scales, out,
+                            ws=self.workspace.get(P.ifq_f8_matmul_workspace_bytes(mm), dev))
         return out
 
 
@@ -161,18 +173,19 @@ class AttentionLayer:
             _check_out(out, x, self.out.n)
         if max_kv is None:
             max_kv = self.max_pages * self.page_tokens
-        rows = self.qkv(x)
-        q = torch.empty(tokens, self.heads * self.head_dim, dtype=x.dtype, device=dev)
-        mixed = torch.empty_like(q)
-        if tokens:
-            k = rows[:, self.heads * self.head_dim:]
-            v = rows[:, (self.heads + self.kv_heads) * self.head_dim:]
-            # the queries lie in the product's rows, and dense once rotated
-            P.ifq_kv_append(self._desc(batch, tokens, max_q, max_kv, x.dtype, rows.shape[1]),
-                            rows, k, v, self.cosines, self.sines, offsets, lengths, pages,
-                            self.cache, q)
-            d = self._desc(batch, tokens, max_q, max_kv, x.dtype)
-            P.ifq_kv_attention(d, q, offsets, lengths, pages, self.cache, mixed,
-                               ws=self.workspace.get(P.ifq_kv_attention_workspace_bytes(d),
-                                                     dev))
-        return self.out(mixed, out=out)
+        with _on(dev):
+            rows = self.qkv(x)
+            q = torch.empty(tokens, self.heads * self.head_dim, dtype=x.dtype, device=dev)
+            mixed = torch.empty_like(q)
+            if tokens:
+                k = rows[:, self.heads * self.head_dim:]
+                v = rows[:, (self.heads + self.kv_heads) * self.head_dim:]
+                # the queries lie in the product's rows, and dense once rotated
+                P.ifq_kv_append(self._desc(batch, tokens, max_q, max_kv, x.dtype, rows.shape[1]),
+                                rows, k, v, self.cosines, self.sines, offsets, lengths, pages,
+                                self.cache, q)
+                d = self._desc(batch, tokens, max_q, max_kv, x.dtype)
+                P.ifq_kv_attention(d, q, offsets, lengths, pages, self.cache, mixed,
+                                   ws=self.workspace.get(P.ifq_kv_attention_workspace_bytes(d),
+                                                         dev))
+            return self.out(mixed, out=out)

@@ -1,5 +1,6 @@
 """The layers' side of the binding, on the CPU, with tensors that only claim to be on
-GPUs: what is not on the layer's GPU is refused before any launch."""
+GPUs: what is not on the layer's GPU is refused before any launch, and launches go to
+that GPU also where another one is torch's current."""
 import pytest
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
@@ -94,3 +95,15 @@ def test_an_output_that_does_not_fit_is_refused_before_the_append(launches, chan
     with pytest.raises(ValueError):
         attend(**args, max_q=3)
     assert launches.seen == []
+
+
+@pytest.mark.parametrize("dev", ["cuda:0", "cuda:1"])
+def test_launches_go_to_the_layers_gpu(launches, dev):
+    attend = layer(dev)
+    attend(**arguments(dev), max_q=3)
+    attend.qkv(torch.empty(5, 64, dtype=BF16, device=dev))
+    assert [n for n, _ in launches.seen] == 2 * ["ifq_f8_quantize"] + [
+        "ifq_f8_quantize", "ifq_f8_matmul", "ifq_kv_append", "ifq_kv_attention",
+        "ifq_f8_quantize", "ifq_f8_matmul", "ifq_f8_quantize", "ifq_f8_matmul"]
+    assert {index for _, index in launches.seen} == {torch.device(dev).index}
+    assert Launches.current == 0
