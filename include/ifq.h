@@ -726,6 +726,7 @@ IFQ_API ifq_status ifq_f8_quantize(const ifq_f8_quant_desc* d, const void* x, vo
  *                2^25)
  *   ld_y         elements from row to row of y, >= n
  *   y_type       IFQ_TYPE_BF16, F16 or F32
+ *   reserved     0
  */
 typedef struct ifq_f8_matmul_desc {
   int64_t m, n, k;

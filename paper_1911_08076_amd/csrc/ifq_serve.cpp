@@ -57,6 +57,8 @@ ifq_status check_matmul(const ifq_f8_matmul_desc* d) {
     return fail(IFQ_ERR_INVALID_ARGUMENT, "product: need m, n in 0..2^30 and k in 1..2^30");
   if (d->y_type != IFQ_TYPE_BF16 && d->y_type != IFQ_TYPE_F16 && d->y_type != IFQ_TYPE_F32)
     return fail(IFQ_ERR_INVALID_ARGUMENT, "product: unknown type %d", d->y_type);
+  if (d->reserved != 0)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "product: reserved must be 0");
   if (d->ld_a < d->k || d->ld_w < d->k || d->ld_y < d->n || d->ld_a > kMaxStride ||
       d->ld_w > kMaxStride || d->ld_y > kMaxStride)
     return fail(IFQ_ERR_INVALID_ARGUMENT, "product: a leading dimension is below its row");

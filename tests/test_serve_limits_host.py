@@ -20,3 +20,13 @@ def test_workspace_with_the_largest_windows_and_sinks(max_q):
     for window, sinks in ((100, 2 ** 31 - 32), (100, 2 ** 31 - 31), (100, INT_MAX),
                           (INT_MAX, 0), (INT_MAX, INT_MAX), (INT_MAX - 31, 5)):
         assert workspace(window, sinks, max_q) == whole, (window, sinks)
+
+
+@pytest.mark.parametrize("value", [1, -1, INT_MAX])
+def test_product_refuses_what_is_reserved(value):
+    d = P.f8_matmul_desc(64, 256, 4096, P.IFQ_TYPE_BF16)
+    d.reserved = value
+    with pytest.raises(P.IfqError) as e:
+        P.ifq_f8_matmul(d, None, None, None, None, None, stream=0)
+    assert e.value.status == -1 and "reserved" in str(e.value)
+    assert P.ifq_f8_matmul_workspace_bytes(d) == 0
