@@ -744,6 +744,13 @@ typedef struct ifq_f8_matmul_desc {
 IFQ_API size_t ifq_f8_matmul_workspace_bytes(const ifq_f8_matmul_desc* d);
 
 /*
+ * Name of the kernel that ifq_f8_matmul launches for d, as a static string: the
+ * symbol without the type of y, or "" for an invalid desc or an empty product.
+ * Host; for profiling, benchmarks and tests.
+ */
+IFQ_API const char* ifq_f8_matmul_kernel_name(const ifq_f8_matmul_desc* d);
+
+/*
  *   a, w               device e4m3 codes [m][ld_a] and [n][ld_w], 16-byte aligned
  *   a_scales           device float [ceil(k/128)][m] (ifq_f8_quantize, block_rows 1)
  *   w_scales           device float [ceil(k/128)][ceil(n/128)] (block_rows 128)
@@ -855,6 +862,12 @@ IFQ_API ifq_status ifq_kv_read(const ifq_kv_desc* d, const int32_t* offsets,
  * order by the one that ends last. Rules as for ifq_conv_workspace_bytes. Host.
  */
 IFQ_API size_t ifq_kv_attention_workspace_bytes(const ifq_kv_desc* d);
+
+/*
+ * Name of the kernel that ifq_kv_attention launches for d, as for
+ * ifq_f8_matmul_kernel_name (without the type of q). Host.
+ */
+IFQ_API const char* ifq_kv_attention_kernel_name(const ifq_kv_desc* d);
 
 /*
  * Attention of the new tokens over their sequences' cached rows:

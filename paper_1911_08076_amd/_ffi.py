@@ -196,11 +196,13 @@ SIGNATURES = [
     ("ifq_static_workspace_bytes", size_t, []),
     ("ifq_f8_quantize", i32, [ctypes.POINTER(F8QuantDesc), vp, vp, vp, vp]),
     ("ifq_f8_matmul_workspace_bytes", size_t, [ctypes.POINTER(F8MatmulDesc)]),
+    ("ifq_f8_matmul_kernel_name", ctypes.c_char_p, [ctypes.POINTER(F8MatmulDesc)]),
     ("ifq_f8_matmul", i32, [ctypes.POINTER(F8MatmulDesc), vp, vp, vp, vp, vp, vp, size_t, vp]),
     ("ifq_kv_cache_bytes", size_t, [ctypes.POINTER(KvDesc)]),
     ("ifq_kv_append", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
     ("ifq_kv_read", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp]),
     ("ifq_kv_attention_workspace_bytes", size_t, [ctypes.POINTER(KvDesc)]),
+    ("ifq_kv_attention_kernel_name", ctypes.c_char_p, [ctypes.POINTER(KvDesc)]),
     ("ifq_kv_attention", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp, size_t, vp]),
 ]
 

@@ -410,6 +410,10 @@ def ifq_f8_matmul_workspace_bytes(desc):
     return int(_lib().ifq_f8_matmul_workspace_bytes(ctypes.byref(desc)))
 
 
+def ifq_f8_matmul_kernel_name(desc):
+    return _lib().ifq_f8_matmul_kernel_name(ctypes.byref(desc)).decode()
+
+
 def ifq_f8_matmul(desc, a, a_scales, w, w_scales, y, ws=None, stream=None):
     """ws None: a zero-filled device workspace is made for this call where it
     needs one, as for ifq_conv_forward."""
@@ -455,6 +459,10 @@ def ifq_kv_read(desc, offsets, lengths, pages, cache, k_out, v_out, stream=None)
 
 def ifq_kv_attention_workspace_bytes(desc):
     return int(_lib().ifq_kv_attention_workspace_bytes(ctypes.byref(desc)))
+
+
+def ifq_kv_attention_kernel_name(desc):
+    return _lib().ifq_kv_attention_kernel_name(ctypes.byref(desc)).decode()
 
 
 def ifq_kv_attention(desc, q, offsets, lengths, pages, cache, out, ws=None, stream=None):

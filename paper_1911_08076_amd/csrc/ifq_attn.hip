@@ -988,6 +988,17 @@ size_t kv_attention_workspace_bytes(const ifq_kv_desc& d) {
          (size_t)p.units * p.splits * p.rows * (d.head_dim + 4) * sizeof(float);
 }
 
+const char* kv_attention_kernel_name(const ifq_kv_desc& d) {
+  static const char* const names[3][4] = {
+      {"kv_attention_many<64>", "kv_attention_few<64, 1>", "kv_attention_few<64, 2>",
+       "kv_attention_few<64, 4>"},
+      {"kv_attention_many<128>", "kv_attention_few<128, 1>", "kv_attention_few<128, 2>",
+       "kv_attention_few<128, 4>"},
+      {"kv_attention_many<256>", "kv_attention_few<256, 1>", "kv_attention_few<256, 2>", ""}};
+  const Plan p = plan_of(d);
+  return names[d.head_dim == 64 ? 0 : d.head_dim == 128 ? 1 : 2][p.few == 4 ? 3 : p.few];
+}
+
 hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs& c, void* out,
                                void* ws, hipStream_t stream) {
   const Plan p = plan_of(d);

@@ -535,25 +535,6 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void f8_matmul_tiled(MatmulAr
   }
 }
 
-template <typename T, int MT>
-void few(const MatmulArgs& a, hipStream_t stream) {
-  const dim3 grid((a.n + 15) / 16, (a.m + 16 * MT - 1) / (16 * MT));
-  const int64_t groups = (int64_t)grid.x * grid.y;
-  if (groups <= 128 && a.kb >= 16)
-    hipLaunchKernelGGL((f8_matmul_few<T, MT, 16>), grid, dim3(1024), 0, stream, a);
-  else if (groups <= 512 && a.kb >= 8)
-    hipLaunchKernelGGL((f8_matmul_few<T, MT, 8>), grid, dim3(512), 0, stream, a);
-  else
-    hipLaunchKernelGGL((f8_matmul_few<T, MT, 4>), grid, dim3(256), 0, stream, a);
-}
-
-template <typename T, int MT, int NT, int WK>
-void tiled(const MatmulArgs& a, hipStream_t stream) {
-  const int gm = (a.m + 64 * MT - 1) / (64 * MT), gn = (a.n + 64 * NT - 1) / (64 * NT);
-  hipLaunchKernelGGL((f8_matmul_tiled<T, MT, NT, 2, 2, WK>), dim3(gm * gn * a.splits),
-                     dim3(256 * WK), 0, stream, a, gm);
-}
-
 constexpr int64_t kSplitGroups = 512;    // workgroups that a split of k aims at
 
 enum Way { kRows16, kRows32, kTiles64, kTiles128 };
@@ -594,23 +575,63 @@ Way way_of(int64_t m, int64_t n, int64_t k) {
   return t64 <= t128 ? kTiles64 : kTiles128;
 }
 
-int64_t splits_of(int64_t m, int64_t n, int64_t k) {
-  if (m == 0 || n == 0 || way_of(m, n, k) != kTiles64) return 1;
-  return parts_of(tiles(m, n, 64, 64), blocks_of(k));
-}
+// Which kernel, and how its work is split.
+struct Plan {
+  Way way;
+  int32_t waves;     // few rows: waves that share k
+  int32_t halves;    // tiles of 128: groups of waves that share k
+  int64_t splits;    // tiles of 64: parts of k
+  int64_t groups;    // workgroups
+};
 
-template <typename T>
-void matmul(const MatmulArgs& a, hipStream_t stream) {
-  switch (way_of(a.m, a.n, a.k)) {
-    case kRows16: return few<T, 1>(a, stream);
-    case kRows32: return few<T, 2>(a, stream);
-    case kTiles64: return tiled<T, 1, 1, 1>(a, stream);
+Plan plan_of(int64_t m, int64_t n, int64_t k) {
+  const int64_t kb = blocks_of(k);
+  Plan p = {way_of(m, n, k), 4, 1, 1, 0};
+  switch (p.way) {
+    case kRows16:
+    case kRows32:
+      p.groups = tiles(m, n, p.way == kRows16 ? 16 : 32, 16);
+      if (p.groups <= 128 && kb >= 16) p.waves = 16;
+      else if (p.groups <= 512 && kb >= 8) p.waves = 8;
+      break;
+    case kTiles64:
+      p.splits = parts_of(tiles(m, n, 64, 64), kb);
+      p.groups = tiles(m, n, 64, 64) * p.splits;
+      break;
     case kTiles128:
+      p.groups = tiles(m, n, 128, 128);
       // alone on its CU a tile waits for its blocks unless two of them are in
       // hand: k in halves 515 x 6144 x 4096 43 -> 38 us, k = 1024 15.6 -> 14.9,
       // k = 512 10.7 -> 11
-      if (tiles(a.m, a.n, 128, 128) <= 256 && a.kb >= 8) return tiled<T, 2, 2, 2>(a, stream);
-      return tiled<T, 2, 2, 1>(a, stream);
+      if (p.groups <= 256 && kb >= 8) p.halves = 2;
+      break;
+  }
+  return p;
+}
+
+template <typename T, int MT>
+void few(const MatmulArgs& a, const Plan& p, hipStream_t stream) {
+  const dim3 grid((a.n + 15) / 16, (a.m + 16 * MT - 1) / (16 * MT)), block(64 * p.waves);
+  if (p.waves == 16) hipLaunchKernelGGL((f8_matmul_few<T, MT, 16>), grid, block, 0, stream, a);
+  else if (p.waves == 8) hipLaunchKernelGGL((f8_matmul_few<T, MT, 8>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((f8_matmul_few<T, MT, 4>), grid, block, 0, stream, a);
+}
+
+template <typename T, int MT, int NT, int WK>
+void tiled(const MatmulArgs& a, const Plan& p, hipStream_t stream) {
+  const int gm = (a.m + 64 * MT - 1) / (64 * MT);
+  hipLaunchKernelGGL((f8_matmul_tiled<T, MT, NT, 2, 2, WK>), dim3((uint32_t)p.groups),
+                     dim3(256 * WK), 0, stream, a, gm);
+}
+
+template <typename T>
+void matmul(const MatmulArgs& a, const Plan& p, hipStream_t stream) {
+  switch (p.way) {
+    case kRows16: return few<T, 1>(a, p, stream);
+    case kRows32: return few<T, 2>(a, p, stream);
+    case kTiles64: return tiled<T, 1, 1, 1>(a, p, stream);
+    case kTiles128:
+      return p.halves == 2 ? tiled<T, 2, 2, 2>(a, p, stream) : tiled<T, 2, 2, 1>(a, p, stream);
   }
 }
 
@@ -634,19 +655,31 @@ hipError_t launch_f8_quantize(const ifq_f8_quant_desc& d, const void* x, void* c
 }
 
 size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d) {
-  const int64_t s = splits_of(d.m, d.n, d.k);
-  return s == 1 ? 0 : kSplitCounterBytes + tiles(d.m, d.n, 64, 64) * s * 64 * 64 * sizeof(float);
+  if (d.m == 0 || d.n == 0) return 0;
+  const Plan p = plan_of(d.m, d.n, d.k);
+  return p.splits == 1 ? 0 : kSplitCounterBytes + p.groups * 64 * 64 * sizeof(float);
 }
 
 int64_t f8_matmul_groups(const ifq_f8_matmul_desc& d) {
-  if (d.m == 0 || d.n == 0) return 0;
-  switch (way_of(d.m, d.n, d.k)) {
-    case kRows16: return tiles(d.m, d.n, 16, 16);
-    case kRows32: return tiles(d.m, d.n, 32, 16);
-    case kTiles64: return tiles(d.m, d.n, 64, 64) * splits_of(d.m, d.n, d.k);
-    case kTiles128: return tiles(d.m, d.n, 128, 128);
+  return d.m == 0 || d.n == 0 ? 0 : plan_of(d.m, d.n, d.k).groups;
+}
+
+const char* f8_matmul_kernel_name(const ifq_f8_matmul_desc& d) {
+  if (d.m == 0 || d.n == 0) return "";
+  const Plan p = plan_of(d.m, d.n, d.k);
+  const int w = p.waves == 16 ? 2 : p.waves == 8 ? 1 : 0;
+  static const char* const rows16[] = {"f8_matmul_few<1, 4>", "f8_matmul_few<1, 8>",
+                                       "f8_matmul_few<1, 16>"};
+  static const char* const rows32[] = {"f8_matmul_few<2, 4>", "f8_matmul_few<2, 8>",
+                                       "f8_matmul_few<2, 16>"};
+  switch (p.way) {
+    case kRows16: return rows16[w];
+    case kRows32: return rows32[w];
+    case kTiles64: return "f8_matmul_tiled<1, 1, 2, 2, 1>";
+    case kTiles128:
+      return p.halves == 2 ? "f8_matmul_tiled<2, 2, 2, 2, 2>" : "f8_matmul_tiled<2, 2, 2, 2, 1>";
   }
-  return 0;
+  return "";
 }
 
 hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a_, const float* a_scales,
@@ -666,14 +699,15 @@ hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a_, const f
   a.k = (int32_t)d.k;
   a.kb = (a.k + kF8Block - 1) / kF8Block;
   a.nb = (a.n + kF8Block - 1) / kF8Block;
-  a.splits = (int32_t)splits_of(d.m, d.n, d.k);
+  const Plan p = plan_of(d.m, d.n, d.k);
+  a.splits = (int32_t)p.splits;
   a.count = static_cast<uint32_t*>(ws);
   a.part = a.splits > 1
                ? reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kSplitCounterBytes)
                : nullptr;
-  if (d.y_type == IFQ_TYPE_BF16) matmul<__bf16>(a, stream);
-  else if (d.y_type == IFQ_TYPE_F16) matmul<_Float16>(a, stream);
-  else matmul<float>(a, stream);
+  if (d.y_type == IFQ_TYPE_BF16) matmul<__bf16>(a, p, stream);
+  else if (d.y_type == IFQ_TYPE_F16) matmul<_Float16>(a, p, stream);
+  else matmul<float>(a, p, stream);
   return hipGetLastError();
 }
 

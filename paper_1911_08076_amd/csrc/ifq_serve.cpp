@@ -169,6 +169,10 @@ size_t ifq_f8_matmul_workspace_bytes(const ifq_f8_matmul_desc* d) {
   return ifq::f8_matmul_workspace_bytes(*d);
 }
 
+const char* ifq_f8_matmul_kernel_name(const ifq_f8_matmul_desc* d) {
+  return check_matmul(d) ? "" : ifq::f8_matmul_kernel_name(*d);
+}
+
 ifq_status ifq_f8_matmul(const ifq_f8_matmul_desc* d, const void* a, const float* a_scales,
                          const void* w, const float* w_scales, void* y, void* ws,
                          size_t ws_bytes, hipStream_t stream) {
@@ -236,6 +240,10 @@ ifq_status ifq_kv_read(const ifq_kv_desc* d, const int32_t* offsets, const int32
 size_t ifq_kv_attention_workspace_bytes(const ifq_kv_desc* d) {
   if (check_kv(d) || nothing(d)) return 0;
   return ifq::kv_attention_workspace_bytes(*d);
+}
+
+const char* ifq_kv_attention_kernel_name(const ifq_kv_desc* d) {
+  return check_kv(d) || nothing(d) ? "" : ifq::kv_attention_kernel_name(*d);
 }
 
 ifq_status ifq_kv_attention(const ifq_kv_desc* d, const void* q, const int32_t* offsets,

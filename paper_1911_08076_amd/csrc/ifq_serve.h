@@ -29,6 +29,7 @@ hipError_t launch_f8_quantize(const ifq_f8_quant_desc& d, const void* x, void* c
 
 size_t f8_matmul_workspace_bytes(const ifq_f8_matmul_desc& d);
 int64_t f8_matmul_groups(const ifq_f8_matmul_desc& d);   // workgroups of its launch
+const char* f8_matmul_kernel_name(const ifq_f8_matmul_desc& d);
 hipError_t launch_f8_matmul(const ifq_f8_matmul_desc& d, const void* a, const float* a_scales,
                             const void* w, const float* w_scales, void* y, void* ws,
                             hipStream_t stream);
@@ -40,6 +41,7 @@ hipError_t launch_kv_read(const ifq_kv_desc& d, const KvArgs& a, void* k_out, vo
                           hipStream_t stream);
 
 size_t kv_attention_workspace_bytes(const ifq_kv_desc& d);
+const char* kv_attention_kernel_name(const ifq_kv_desc& d);
 hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs& a, void* out,
                                void* ws, hipStream_t stream);
 
