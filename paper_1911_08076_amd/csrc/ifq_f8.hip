@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ifq_serve.h"
 
@@ -209,6 +210,27 @@ __device__ __forceinline__ f16x8 halves(uint32_t a, uint32_t b) {
   return f16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
+// Adds the sum of a block of 128 times the block's two scales: as one factor, where
+// fp32 holds sa * sw as a normal number. Where it is below those or infinite the
+// larger scale comes first: the result may be well within the range all the same
+// (scales of 2^-80 and 2^-65 with a sum of 2^20).
+__device__ __forceinline__ bool out_of_range(float f) {
+  return __builtin_amdgcn_classf(f, 0x2F4);       // not normal, and no NaN
+}
+
+struct Scales {
+  float first, then;
+  __device__ __forceinline__ Scales(float sa, float sw) {
+    const float one = sa * sw;
+    const bool out = out_of_range(one), a = __builtin_fabsf(sa) > __builtin_fabsf(sw);
+    first = out ? (a ? sa : sw) : 1.0f;
+    then = out ? (a ? sw : sa) : one;
+  }
+  __device__ __forceinline__ float add(float acc, float sum) const {
+    return __builtin_fmaf(sum * first, then, acc);
+  }
+};
+
 // Four sums of a row of y, or what is left of it; a row may begin at any element.
 template <typename T>
 __device__ __forceinline__ void store4(T* p, f32x4 v, int left) {
@@ -287,9 +309,9 @@ __global__ __launch_bounds__(64 * KS) void f8_matmul_few(MatmulArgs a) {
         }
 #pragma unroll
       for (int x = 0; x < MT; ++x) {
-        const float f = sa[i][x] * sw[i];
+        const Scales f(sa[i][x], sw[i]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[x][e] = __builtin_fmaf(part[x][e], f, acc[x][e]);
+        for (int e = 0; e < 4; ++e) acc[x][e] = f.add(acc[x][e], part[x][e]);
       }
       if (b + AHEAD * KS < a.kb) load(b + AHEAD * KS, i);
     }
@@ -410,10 +432,6 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void f8_matmul_tiled(MatmulAr
   for (int x = 0; x < MT; ++x) m[x] = min(m0 + wm + 32 * x + r, a.m - 1);
   const int nblock = min((n0 + wn) / kF8Block, a.nb - 1);
   v16f acc[MT][NT];
-#pragma unroll
-  for (int x = 0; x < MT; ++x)
-#pragma unroll
-    for (int z = 0; z < NT; ++z) acc[x][z] = v16f{};
   // the scales of a block come a block ahead, as its rows do
   float sa[MT], sw;
   auto load_scales = [&](int b) {
@@ -421,61 +439,87 @@ __global__ __launch_bounds__(64 * WM * WN * WK, 2) void f8_matmul_tiled(MatmulAr
 #pragma unroll
     for (int x = 0; x < MT; ++x) sa[x] = a.sa[(int64_t)b * a.m + m[x]];
   };
-  if (b0 + half < b1) {
-    load(b0 + half, 2 * half);
-    load_scales(b0 + half);
-  }
-  int turn = 0;
-  for (int b = b0 + half; b < b1 + half; b += WK, turn ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    float f[MT];
+  // All blocks with sa * sw as one factor; whether one left the range is noted, and
+  // then the tile is summed again with two (TWO). With that the products take 1 %
+  // longer than with one factor whatever it is; a branch for each block: 3 to 10 %.
+  __shared__ int again;
+  if (threadIdx.x == 0) again = 0;
+  auto sum = [&](auto two) {
+    constexpr bool TWO = decltype(two)::value;
+    bool out = false;
 #pragma unroll
-    for (int x = 0; x < MT; ++x) f[x] = sa[x] * sw;
-    if (WK > 1 && b >= b1) break;          // the last wait of a half with a block less
-    if (b + WK < b1) {
-      load(b + WK, 2 * half + (turn ^ 1));
-      load_scales(b + WK);
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+      for (int z = 0; z < NT; ++z) acc[x][z] = v16f{};
+    if (b0 + half < b1) {
+      load(b0 + half, 2 * half);
+      load_scales(b0 + half);
     }
-    // ahead of a wave of the other workgroup that still waits for its block
-    // (8192 x 14336 x 4096: 878 -> 852 us)
-    __builtin_amdgcn_s_setprio(1);
-    const uint8_t(*at)[kF8Block] = lds[2 * half + turn];
-    // a lane's cells: 2 j + h of its row
-    f16x8 wh[NT][8];
+    int turn = 0;
+    for (int b = b0 + half; b < b1 + half; b += WK, turn ^= 1) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      const float fw = sw;
+      float fa[MT];
 #pragma unroll
-    for (int z = 0; z < NT; ++z)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(
-            &at[TM + wn + 32 * z + r][16 * ((2 * j + h) ^ (r >> 1 & 7))]);
-        wh[z][2 * j] = halves(v[0], v[1]);
-        wh[z][2 * j + 1] = halves(v[2], v[3]);
+      for (int x = 0; x < MT; ++x) {
+        fa[x] = sa[x];
+        if (!TWO) out |= out_of_range(fa[x] * fw);
       }
-#pragma unroll
-    for (int x = 0; x < MT; ++x) {
-      v16f part[NT];
-#pragma unroll
-      for (int z = 0; z < NT; ++z) part[z] = v16f{};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(
-            &at[wm + 32 * x + r][16 * ((2 * j + h) ^ (r >> 1 & 7))]);
-        const f16x8 a0 = halves(v[0], v[1]), a1 = halves(v[2], v[3]);
-#pragma unroll
-        for (int z = 0; z < NT; ++z) {
-          part[z] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wh[z][2 * j], a0, part[z], 0, 0, 0);
-          part[z] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wh[z][2 * j + 1], a1, part[z], 0, 0, 0);
-        }
+      if (WK > 1 && b >= b1) break;          // the last wait of a half with a block less
+      if (b + WK < b1) {
+        load(b + WK, 2 * half + (turn ^ 1));
+        load_scales(b + WK);
       }
+      // ahead of a wave of the other workgroup that still waits for its block
+      // (8192 x 14336 x 4096: 878 -> 852 us)
+      __builtin_amdgcn_s_setprio(1);
+      const uint8_t(*at)[kF8Block] = lds[2 * half + turn];
+      // a lane's cells: 2 j + h of its row
+      f16x8 wh[NT][8];
 #pragma unroll
       for (int z = 0; z < NT; ++z)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          acc[x][z][e] = __builtin_fmaf(part[z][e], f[x], acc[x][z][e]);
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(
+              &at[TM + wn + 32 * z + r][16 * ((2 * j + h) ^ (r >> 1 & 7))]);
+          wh[z][2 * j] = halves(v[0], v[1]);
+          wh[z][2 * j + 1] = halves(v[2], v[3]);
+        }
+#pragma unroll
+      for (int x = 0; x < MT; ++x) {
+        v16f part[NT];
+#pragma unroll
+        for (int z = 0; z < NT; ++z) part[z] = v16f{};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(
+              &at[wm + 32 * x + r][16 * ((2 * j + h) ^ (r >> 1 & 7))]);
+          const f16x8 a0 = halves(v[0], v[1]), a1 = halves(v[2], v[3]);
+#pragma unroll
+          for (int z = 0; z < NT; ++z) {
+            part[z] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wh[z][2 * j], a0, part[z],
+                                                             0, 0, 0);
+            part[z] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wh[z][2 * j + 1], a1, part[z],
+                                                             0, 0, 0);
+          }
+        }
+        const Scales f(fa[x], fw);
+        const float one = fa[x] * fw;
+#pragma unroll
+        for (int z = 0; z < NT; ++z)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            acc[x][z][e] = TWO ? f.add(acc[x][z][e], part[z][e])
+                               : __builtin_fmaf(part[z][e], one, acc[x][z][e]);
+      }
+      __builtin_amdgcn_s_setprio(0);
     }
-    __builtin_amdgcn_s_setprio(0);
-  }
+    return out;
+  };
+  if (sum(std::false_type{})) again = 1;
+  __syncthreads();
+  if (again) sum(std::true_type{});
   if constexpr (WK > 1) {
     static_assert(sizeof(lds) >= sizeof(float) * 64 * WAVES * MT * NT * 16, "");
     __syncthreads();
