@@ -814,7 +814,9 @@ IFQ_API ifq_status ifq_f8_matmul(const ifq_f8_matmul_desc* d, const void* a,
  *   pages    int32 [batch][max_pages]: where its positions page_tokens*s .. are
  * A position outside the page table, or on a page outside 0..num_pages-1, is
  * not stored, reads as 0 and is not visible. Two sequences must not append to
- * the same 32 tokens of a page in one call.
+ * the same 32 tokens of a page in one call. Rows of no sequence (before offsets[0]
+ * and from offsets[batch] on, and those beyond max_q of one) are neither read nor
+ * written, in the inputs and in the outputs.
  */
 typedef struct ifq_kv_desc {
   int32_t batch, total_q, max_q, max_kv;
@@ -874,7 +876,8 @@ IFQ_API const char* ifq_kv_attention_kernel_name(const ifq_kv_desc* d);
  *   out[i] = sum over visible j of softmax_j(scale * q[i].k[j]) v[j]
  * with k, v the values that the rows stand for, scores and sums in fp32. Query
  * head h reads key/value head h / (heads / kv_heads). A query that sees
- * nothing gives 0.
+ * nothing gives 0. Sums run with codes up to 31 and weights up to 2^8: values up
+ * to 2^98 stay finite in sequences of up to 2^20 tokens.
  *   q      device [total_q][q_stride], 16-byte aligned
  *   out    device [total_q][o_stride], 16-byte aligned
  *   ws     workspace of ws_bytes >= ifq_kv_attention_workspace_bytes(d)

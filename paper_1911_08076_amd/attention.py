@@ -157,8 +157,9 @@ class AttentionLayer:
         sequence after another; offsets int32 [batch + 1], lengths int32 [batch]
         (with the new tokens) and pages int32 [batch][max_pages] as for
         ifq_kv_append; max_q: the most new tokens of a sequence; max_kv: about how
-        long the longest sequence is, for the split of the work. Returns
-        [tokens][hidden]."""
+        long the longest sequence is, for the split of the work (None: as long as
+        the page table allows). Returns [tokens][hidden]; a row of no sequence holds
+        anything."""
         dev = self.cache.device
         _check_rows(x, self.qkv.k, (torch.bfloat16, torch.float16), dev)
         tokens, batch = x.shape[0], lengths.numel()
