@@ -782,7 +782,8 @@ IFQ_API ifq_status ifq_f8_matmul(const ifq_f8_matmul_desc* d, const void* a,
  *
  *   batch        sequences
  *   total_q      rows of new tokens (queries), over all sequences
- *   max_q        the most new tokens of one sequence
+ *   max_q        the most new tokens of one sequence; the attention's kernel goes by
+ *                it, so that prompts and single tokens run faster in calls of their own
  *   max_kv       about how long the longest sequence is; only the split of
  *                the work goes by it, any value >= 0 gives the same result
  *   heads, kv_heads, head_dim

@@ -3,7 +3,8 @@ operators: the inputs and weights of its products in 8-bit floats, the keys and
 values of past tokens in a paged cache of 4-bit codes.
 
 A step takes the new tokens of a batch of sequences, one each (decoding) or many
-(prompts), and makes six calls on the current stream: quantize, product to
+(prompts; both in one step give the same, but take longer than a step each), and
+makes six calls on the current stream: quantize, product to
 queries, keys and values, append (with the rotation), attention, quantize,
 product. Nothing in it waits for the GPU or reads the sequences' lengths on the
 host, so a step on fixed inputs can be captured in a graph.

@@ -577,9 +577,11 @@ __device__ __forceinline__ void join_parts(const AttnArgs& a, const Seq& s, int 
 // step of its part of the sequence for the same rows, and join their results
 // in LDS. Bound by memory where all CUs have work: 5 sequences of up to 120001
 // tokens, 8 heads of 128, 78.5 us, 4.8 TB/s (vector instructions take 40 % of the
-// time, the products 17 %). A step of a wave alone on its SIMD takes 2.4 us for
-// 128 tokens of 128 dims, which is what short sequences see: one of 1111 tokens
-// 9.3 us, of which an empty call is 7. With all U blocks in one step of 16
+// time, the products 17 %); 5 of up to 60000, 4 heads of 256, 62 us, 3.0 TB/s, with
+// one workgroup on a CU. A step of a wave alone on its SIMD takes 2.4 us for 128
+// tokens of 128 dims, which is what short sequences see: one of 1111 tokens takes
+// 8.8 to 9.8 us on the GPU, where the shortest kernel takes 2: the step, then the
+// join of three parts through memory. With all U blocks in one step of 16
 // columns, rows in use grow from 16 / U to 16 in the softmax; a block's products
 // still run over all 16 columns, at a quarter of their use for U = 4.
 template <typename T, int D, int U>
@@ -662,11 +664,13 @@ struct Stage {
 // while one is computed on, the next one's codes are on their way into
 // registers. The last rows, which see most, come first.
 // Bound by vector instructions beside the products: prompts of 900 to 2048
-// tokens over up to 6100, 32 heads of 128, 417 us = 612 TFLOP/s of 4 D a pair,
-// with vector instructions at 56 % and products at 39 % of the cycles. The two
-// halves of p t make 3 products' work of 2 (it buys 16 bits of p t and fp32's
-// range). With the codes expanded by each wave for itself, without LDS, the same
-// prompts took 772 us.
+// tokens over up to 6100, 32 heads of 128, 412 us = 620 TFLOP/s of 4 D a pair
+// (472 at first in a row of calls, as the clocks rise), with vector instructions at
+// 56 % and products at 40 % of the cycles. 32 heads of 64: 332 us, 384 TFLOP/s; 16
+// of 256, of which registers and LDS hold one query tile a wave and one workgroup a
+// CU: 824 us, 310 TFLOP/s. The two halves of p t make 3 products' work of 2 (it buys
+// 16 bits of p t and fp32's range). With the codes expanded by each wave for
+// itself, without LDS, the first prompts took 772 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnArgs a) {
   typedef Half<T> H;
@@ -891,7 +895,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many(AttnA
 // Blocks of 32 tokens that n tokens fill.
 int64_t code_blocks(int64_t n) { return (n + kCodeTokens - 1) / kCodeTokens; }
 
-// Which kernel, and how its work is split.
+// Which kernel, and how its work is split: by the longest of the sequences, for all
+// of them. A prompt among single tokens takes these along as rows of the kernel for
+// many (512 tokens beside 31 single ones over 32000: 3000 us; as two calls 26 and 202).
 struct Plan {
   int32_t few;            // blocks of a step for few rows (U), 0: many rows
   int32_t row_blocks, splits, chunk;

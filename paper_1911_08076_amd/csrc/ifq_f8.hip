@@ -87,9 +87,10 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
 // registers between the search for the largest and the coding. ROWS = 16: a
 // workgroup takes 16 rows x 4 blocks, so that the scales, which run along the
 // rows, are written 64 bytes at a time; ROWS = 1: 16 blocks of one row.
-// Bound by memory: 8192 x 14336 bfloat16 values 73 us, 4.9 TB/s (a copy of 4 GiB
-// reaches 4.64), with vector instructions on 81 % of the cycles; one row of 4096
-// takes 2.0 us on the GPU, the latency of a launch.
+// Bound by memory: 8192 x 14336 bfloat16 values 73 us, 4.9 TB/s (a copy reaches 4.6
+// to 4.7; after some fifteen calls in a row 85 to 100 us), with vector instructions
+// on 81 % of the cycles; one row of 4096 takes 2.1 us on the GPU, the latency of a
+// launch.
 template <typename T, int ROWS>
 __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
   constexpr int PER = ROWS == 16 ? 4 : 1;
@@ -115,7 +116,8 @@ __global__ __launch_bounds__(256) void f8_quantize_rows(QuantArgs a) {
 }
 
 // A scale per 128 x 128: a workgroup holds the block in registers, 64 values to
-// a thread, so that it too is read once. For weights, when they are loaded.
+// a thread, so that it too is read once. For weights, when they are loaded. Bound by
+// memory: 14336 x 4096 bfloat16 values 38.7 us, 4.6 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void f8_quantize_blocks(QuantArgs a) {
   __shared__ uint32_t part[4];
@@ -177,11 +179,12 @@ hipError_t quantize(QuantArgs a, int block_rows, hipStream_t stream) {
 
 // --- product --------------------------------------------------------------------
 //
-// The products go through the 16-bit matrix instructions, whose sums are
-// fp32: the 8-bit ones keep some 16 bits below the largest product (measured:
-// 1.5e-5 of the result's norm over 128 normal values, against 1e-8), which is
-// too few for a result in fp32. Every e4m3 value is a 16-bit float, and a
-// conversion of two codes is one instruction.
+// The products go through the 16-bit matrix instructions, whose sums are fp32,
+// as the definition has them for every type of y. The 8-bit ones would run at twice
+// the rate, but keep some 16 bits below the largest product (1.5e-5 of the result's
+// norm over 128 normal values, against 1e-8): below what rounds a bfloat16 or a
+// float16 result, but not sums in fp32, so they are not used. Every e4m3 value is a
+// 16-bit float, and a conversion of two codes is one instruction.
 //
 // The weights are the first operand and the activations the second: a lane's
 // sums then belong to one activation row, whose scale is one number, and the
@@ -364,10 +367,11 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
 // c ^ (r & 7) they met in pairs, 4 cycles for each read.
 //
 // Bound by the matrix instructions and the conversions beside them: 8192 x
-// 14336 x 4096 takes 860 to 930 us, 1.03 to 1.12 PFLOP/s (a bfloat16 product of
-// 8192^3 reaches 1.47 here), with products on 54 to 56 % and vector instructions
-// on 53 to 55 % of the cycles, at 1.7 GHz. Tiles of 128 x 128 on 4 waves: a wave
-// converts 128 rows' codes for 64 x 64 sums. 128 x 256 was equal, 192 x 256 and
+// 14336 x 4096 takes 875 us, 1.10 PFLOP/s (860 to 1100 us as the clocks move; a
+// bfloat16 product of 8192^3 reaches 1.47 in a short run and 1.19 twenty times in a
+// row), with products and vector instructions on 55 % of the cycles each, at 1.9
+// GHz. Tiles of 128 x 128 on 4 waves: a wave converts 128 rows' codes for 64 x 64
+// sums. 128 x 256 was equal, 192 x 256 and
 // 256 x 256 spilled registers; three and four blocks in LDS were no faster than
 // two.
 //
