@@ -764,7 +764,7 @@ IFQ_API ifq_status ifq_f8_matmul(const ifq_f8_matmul_desc* d, const void* a,
 /*
  * A paged cache of keys and values in 4-bit codes, and a batch of sequences
  * in it. A row x (one token's key or value of one head) is held as
- *   offset o = min(x) rounded down to bfloat16,
+ *   offset o = min(x) rounded down to bfloat16 (-0 counts below 0),
  *   step   t = ((max(x) - o) / 15) rounded up to bfloat16,
  *   codes  c = rint((x - o) / t) in 0..15        (fp32; t = 0: codes 0)
  * and stands for o + t*c. A row with a NaN or an infinity, or whose spread

@@ -75,6 +75,8 @@ def row_codes(x):
     x = np.ascontiguousarray(x, F)
     with np.errstate(all="ignore"):
         lo, hi = x.min(-1), x.max(-1)
+        # -0 is below 0, wherever in the row it is
+        lo = np.where((lo == 0) & ((x == 0) & np.signbit(x)).any(-1), F(-0.0), lo)
         o = np.ascontiguousarray(lo).view(np.uint32)
         o = np.where(o >> 31, o + np.uint32(0xFFFF), o) & np.uint32(0xFFFF0000)
         off = _f32_of(o)
