@@ -888,6 +888,161 @@ IFQ_API ifq_status ifq_kv_attention(const ifq_kv_desc* d, const void* q, const i
                                     const void* cache, void* out, void* ws, size_t ws_bytes,
                                     hipStream_t stream);
 
+/* -------------------------------------------------------------------------
+ * What follows a decoder's attention: weights in 4-bit floats with a scale per
+ * 32, the products with them, and log probabilities of tokens. Errors and streams
+ * as above.
+ *
+ * A weight is a code of 4 bits (e2m1: sign, 2 exponent bits, 1 mantissa bit;
+ * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6) times its group's scale, a byte s that
+ * stands for 2^(s-127), 255 for NaN. A row's codes lie two in a byte, the first
+ * column in the low half, 16 bytes for a group of 32 columns. The scales lie
+ * [ceil(k/128)][rows][4]: the four groups of 128 columns of a row together.
+ * ------------------------------------------------------------------------- */
+
+/*
+ *   rows, k      the matrix; both may be 0 (nothing is done)
+ *   ld_x         elements from row to row of the values, >= k
+ *   ld_codes     bytes from row to row of the codes, a multiple of 16 that holds
+ *                16 * ceil(k/32)
+ *   x_type       of the values: IFQ_TYPE_BF16, F16 or F32
+ *   reserved     0
+ */
+typedef struct ifq_f4_weights_desc {
+  int64_t rows, k;
+  int64_t ld_x, ld_codes;
+  int32_t x_type, reserved;
+} ifq_f4_weights_desc;
+
+/*
+ * Quantizer: a group's scale is the smallest 2^e with all |x| <= 7 * 2^e, so that no
+ * value is further than half a step from its code (the largest |x| of a group
+ * counts as 2^-96 at least); the code is the nearest to x / 2^e, ties to the even
+ * code, beyond 6 to 6. A group that holds a NaN or an infinity gets the scale NaN
+ * and codes 0. Codes of columns from k up to the next multiple of 32 become 0,
+ * groups past k the smallest scale.
+ *   x        device [rows][ld_x], aligned to its element
+ *   codes    device [rows][ld_codes], 16-byte aligned
+ *   scales   device uint8 [ceil(k/128)][rows][4], 4-byte aligned
+ */
+IFQ_API ifq_status ifq_f4_quantize(const ifq_f4_weights_desc* d, const void* x, void* codes,
+                                   void* scales, hipStream_t stream);
+
+/*
+ * The values that codes and scales stand for, rounded to x's type: exact in
+ * bfloat16 and float32, whose overflow (codes of 4 and more under 2^126 and 2^127) is
+ * infinite, and in float16 from 2^-24 to 65504. Codes that end in columns past k and
+ * scales of groups past k may be anything.
+ */
+IFQ_API ifq_status ifq_f4_dequantize(const ifq_f4_weights_desc* d, const void* codes,
+                                     const void* scales, void* x, hipStream_t stream);
+
+#define IFQ_ACT_NONE 0
+#define IFQ_ACT_SILU 1      /* g / (1 + e^-g) */
+#define IFQ_ACT_GELU 2      /* g/2 (1 + erf(g / sqrt 2)) */
+#define IFQ_ACT_GELU_TANH 3 /* g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) */
+
+/*
+ * Products of 16-bit activations x [m][k] with weights of n rows in 4-bit floats.
+ *   m, n, k      m or n may be 0; k >= 1
+ *   ld_x         elements from row to row of x, >= k
+ *   ld_w         bytes from row to row of the codes, a multiple of 16 that holds
+ *                16 * ceil(k/32) (UNSUPPORTED above 2^25)
+ *   ld_y         elements from row to row of y, >= n
+ *   x_type       IFQ_TYPE_BF16 or F16
+ *   y_type       IFQ_TYPE_BF16, F16 or F32
+ *   activation   IFQ_ACT_NONE for ifq_f4_matmul, one of the others for ifq_f4_gated
+ *   reserved     0
+ */
+typedef struct ifq_f4_matmul_desc {
+  int64_t m, n, k;
+  int64_t ld_x, ld_w, ld_y;
+  int32_t x_type, y_type, activation, reserved;
+} ifq_f4_matmul_desc;
+
+/*
+ * Device workspace bytes of ifq_f4_matmul and of ifq_f4_gated for d (may be 0).
+ * Rules as for ifq_f8_matmul_workspace_bytes. Host.
+ */
+IFQ_API size_t ifq_f4_matmul_workspace_bytes(const ifq_f4_matmul_desc* d);
+IFQ_API size_t ifq_f4_gated_workspace_bytes(const ifq_f4_matmul_desc* d);
+
+/*
+ * Names of the kernels that ifq_f4_matmul and ifq_f4_gated launch for d, as for
+ * ifq_f8_matmul_kernel_name (without the type of x). Host.
+ */
+IFQ_API const char* ifq_f4_matmul_kernel_name(const ifq_f4_matmul_desc* d);
+IFQ_API const char* ifq_f4_gated_kernel_name(const ifq_f4_matmul_desc* d);
+
+/*
+ *   y[i][j] = sum over k of x[i][k] * w[j][k]
+ * with w the values that codes and scales stand for in x's type (float16: rounded
+ * where they are below 2^-24 or above 65504), sums in fp32, rounded once to y's type.
+ * Codes of columns past k and scales of groups past k may be anything.
+ *   x          device [m][ld_x], aligned to its element
+ *   w          device codes [n][ld_w], 16-byte aligned
+ *   w_scales   device uint8 [ceil(k/128)][n][4], 4-byte aligned
+ *   y          device [m][ld_y], aligned to its element; must not overlap the inputs
+ *   ws         workspace of ws_bytes >= ifq_f4_matmul_workspace_bytes(d)
+ */
+IFQ_API ifq_status ifq_f4_matmul(const ifq_f4_matmul_desc* d, const void* x, const void* w,
+                                 const void* w_scales, void* y, void* ws, size_t ws_bytes,
+                                 hipStream_t stream);
+
+/*
+ * The first half of a gated feed-forward block, in one kernel:
+ *   y[i][j] = act(sum over k of x[i][k] * w_gate[j][k]) * sum over k of x[i][k] * w_up[j][k]
+ * with the sums, the activation and the product in fp32, rounded once to y's type.
+ * Arguments as for ifq_f4_matmul; both weights have ld_w.
+ */
+IFQ_API ifq_status ifq_f4_gated(const ifq_f4_matmul_desc* d, const void* x, const void* w_gate,
+                                const void* gate_scales, const void* w_up, const void* up_scales,
+                                void* y, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Log probabilities from logits: with p = softmax(scale * x) over the n values of a
+ * row, the log probability of a given token, the entropy -sum p ln p, and the tokens
+ * of the largest logits, the largest first, equal ones by the lower index.
+ *   rows, n      rows may be 0; n >= 1
+ *   ld_x         elements from row to row of the logits, >= n
+ *   ld_top       elements from row to row of top_logprobs and top_tokens, >= top
+ *   x_type       IFQ_TYPE_BF16, F16 or F32
+ *   top          0..64, at most n
+ *   scale        0 < scale <= 2^64: one over the temperature
+ *   reserved     0
+ */
+typedef struct ifq_logprobs_desc {
+  int64_t rows, n;
+  int64_t ld_x, ld_top;
+  int32_t x_type, top;
+  float scale;
+  int32_t reserved;
+} ifq_logprobs_desc;
+
+/*
+ * Device workspace bytes of ifq_logprobs for d (may be 0): where rows are few they are
+ * split over workgroups. Rules as for ifq_f8_matmul_workspace_bytes. Host.
+ */
+IFQ_API size_t ifq_logprobs_workspace_bytes(const ifq_logprobs_desc* d);
+
+/*
+ *   logits         device [rows][ld_x], aligned to its element; -infinity: a token that
+ *                  cannot be. A row of these alone gives log probabilities of -infinity
+ *                  and the entropy 0. A row with a NaN or +infinity has no distribution:
+ *                  its log probabilities and entropy are NaN, its top tokens -1
+ *   tokens         device int32 [rows]. A negative one stands for no token and gives 0,
+ *                  one from n on NaN
+ *   logprob        device float [rows]; tokens and logprob are NULL together
+ *   entropy        device float [rows], nullable
+ *   top_logprobs   device float [rows][ld_top], top_tokens device int32 likewise;
+ *                  NULL iff top is 0
+ *   ws             workspace of ws_bytes >= ifq_logprobs_workspace_bytes(d)
+ */
+IFQ_API ifq_status ifq_logprobs(const ifq_logprobs_desc* d, const void* logits,
+                                const int32_t* tokens, float* logprob, float* entropy,
+                                float* top_logprobs, int32_t* top_tokens, void* ws,
+                                size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

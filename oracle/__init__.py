@@ -15,6 +15,8 @@ the GPU library:
   layout.py      the 2-bit packed code layout (4 codes per byte along C)
   serve.py       the operators for serving language models: 8-bit float codes
                  and their product, the cache of 4-bit codes, attention
+  f4.py          weights in 4-bit floats, the products with them, activations
+  logprobs.py    log probabilities of given tokens, entropy, top tokens
 
 Parity status per function (what pins it is in the tests):
   conv acc       pinned: brute force, float64 conv2d of integer tensors,

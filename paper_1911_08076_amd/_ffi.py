@@ -47,6 +47,11 @@ IFQ_TYPE_BF16 = 0
 IFQ_TYPE_F16 = 1
 IFQ_TYPE_F32 = 2
 
+IFQ_ACT_NONE = 0
+IFQ_ACT_SILU = 1
+IFQ_ACT_GELU = 2
+IFQ_ACT_GELU_TANH = 3
+
 i32 = ctypes.c_int32
 i64 = ctypes.c_int64
 f32 = ctypes.c_float
@@ -118,6 +123,22 @@ class KvDesc(ctypes.Structure):
                 ("window", i32), ("sinks", i32), ("rot_dim", i32), ("rot_adjacent", i32),
                 ("rot_len", i32), ("scale", f32), ("q_stride", i64), ("k_stride", i64),
                 ("v_stride", i64), ("o_stride", i64)]
+
+
+class F4WeightsDesc(ctypes.Structure):
+    _fields_ = [("rows", i64), ("k", i64), ("ld_x", i64), ("ld_codes", i64),
+                ("x_type", i32), ("reserved", i32)]
+
+
+class F4MatmulDesc(ctypes.Structure):
+    _fields_ = [("m", i64), ("n", i64), ("k", i64), ("ld_x", i64), ("ld_w", i64),
+                ("ld_y", i64), ("x_type", i32), ("y_type", i32), ("activation", i32),
+                ("reserved", i32)]
+
+
+class LogprobsDesc(ctypes.Structure):
+    _fields_ = [("rows", i64), ("n", i64), ("ld_x", i64), ("ld_top", i64),
+                ("x_type", i32), ("top", i32), ("scale", f32), ("reserved", i32)]
 
 
 def address(t):
@@ -204,6 +225,18 @@ SIGNATURES = [
     ("ifq_kv_attention_workspace_bytes", size_t, [ctypes.POINTER(KvDesc)]),
     ("ifq_kv_attention_kernel_name", ctypes.c_char_p, [ctypes.POINTER(KvDesc)]),
     ("ifq_kv_attention", i32, [ctypes.POINTER(KvDesc), vp, vp, vp, vp, vp, vp, vp, size_t, vp]),
+    ("ifq_f4_quantize", i32, [ctypes.POINTER(F4WeightsDesc), vp, vp, vp, vp]),
+    ("ifq_f4_dequantize", i32, [ctypes.POINTER(F4WeightsDesc), vp, vp, vp, vp]),
+    ("ifq_f4_matmul_workspace_bytes", size_t, [ctypes.POINTER(F4MatmulDesc)]),
+    ("ifq_f4_gated_workspace_bytes", size_t, [ctypes.POINTER(F4MatmulDesc)]),
+    ("ifq_f4_matmul_kernel_name", ctypes.c_char_p, [ctypes.POINTER(F4MatmulDesc)]),
+    ("ifq_f4_gated_kernel_name", ctypes.c_char_p, [ctypes.POINTER(F4MatmulDesc)]),
+    ("ifq_f4_matmul", i32, [ctypes.POINTER(F4MatmulDesc), vp, vp, vp, vp, vp, size_t, vp]),
+    ("ifq_f4_gated", i32, [ctypes.POINTER(F4MatmulDesc), vp, vp, vp, vp, vp, vp, vp, size_t,
+                           vp]),
+    ("ifq_logprobs_workspace_bytes", size_t, [ctypes.POINTER(LogprobsDesc)]),
+    ("ifq_logprobs", i32, [ctypes.POINTER(LogprobsDesc), vp, vp, vp, vp, vp, vp, vp, size_t,
+                           vp]),
 ]
 
 # the launching entry points that api.py calls through _ifqcall, in the order
@@ -211,7 +244,8 @@ SIGNATURES = [
 CALLED = ["ifq_conv_forward", "ifq_conv_forward_fp4", "ifq_conv_pool_forward",
           "ifq_conv_pool_forward_fp4", "ifq_maxpool_codes", "ifq_convert_codes",
           "ifq_run_stack", "ifq_run_stack_static", "ifq_f8_quantize", "ifq_f8_matmul",
-          "ifq_kv_append", "ifq_kv_read", "ifq_kv_attention"]
+          "ifq_kv_append", "ifq_kv_read", "ifq_kv_attention", "ifq_f4_quantize",
+          "ifq_f4_dequantize", "ifq_f4_matmul", "ifq_f4_gated", "ifq_logprobs"]
 
 _lib = None
 call = None     # the _ifqcall module, bound to the library

@@ -12,7 +12,7 @@ import numpy as np
 
 from . import _ffi
 from ._ffi import (ConvDesc, FoldParams, JoinParams, Join, PoolDesc, Stack,
-                   F8QuantDesc, F8MatmulDesc, KvDesc,
+                   F8QuantDesc, F8MatmulDesc, KvDesc, F4WeightsDesc, F4MatmulDesc, LogprobsDesc,
                    IFQ_OK, IFQ_JOIN_NONE, IFQ_MAX_THRESHOLDS)
 
 
@@ -475,3 +475,93 @@ def ifq_kv_attention(desc, q, offsets, lengths, pages, cache, out, ws=None, stre
                                     st)
     if rc:
         _check(rc, "ifq_kv_attention")
+
+
+# -- weights in 4-bit floats, and log probabilities -------------------------------
+def f4_weights_desc(rows, k, x_type, ld_x=None, ld_codes=None):
+    """ld_codes None: 16 bytes for each group of 32 columns."""
+    return F4WeightsDesc(rows, k, k if ld_x is None else ld_x,
+                         -(-k // 32) * 16 if ld_codes is None else ld_codes, x_type, 0)
+
+
+def f4_matmul_desc(m, n, k, x_type, y_type=None, ld_x=None, ld_w=None, ld_y=None,
+                   activation=_ffi.IFQ_ACT_NONE):
+    """y_type None: x's; ld_w None: 16 bytes for each group of 32 columns."""
+    return F4MatmulDesc(m, n, k, k if ld_x is None else ld_x,
+                        -(-k // 32) * 16 if ld_w is None else ld_w,
+                        n if ld_y is None else ld_y, x_type,
+                        x_type if y_type is None else y_type, activation, 0)
+
+
+def logprobs_desc(rows, n, x_type, top=0, scale=1.0, ld_x=None, ld_top=None):
+    return LogprobsDesc(rows, n, n if ld_x is None else ld_x, top if ld_top is None else ld_top,
+                        x_type, top, scale, 0)
+
+
+def ifq_f4_quantize(desc, x, codes, scales, stream=None):
+    rc = _ffi.call.f4_quantize(_struct(desc, F4WeightsDesc), x, codes, scales, _stream(stream))
+    if rc:
+        _check(rc, "ifq_f4_quantize")
+
+
+def ifq_f4_dequantize(desc, codes, scales, x, stream=None):
+    rc = _ffi.call.f4_dequantize(_struct(desc, F4WeightsDesc), codes, scales, x, _stream(stream))
+    if rc:
+        _check(rc, "ifq_f4_dequantize")
+
+
+def ifq_f4_matmul_workspace_bytes(desc):
+    return int(_lib().ifq_f4_matmul_workspace_bytes(ctypes.byref(desc)))
+
+
+def ifq_f4_gated_workspace_bytes(desc):
+    return int(_lib().ifq_f4_gated_workspace_bytes(ctypes.byref(desc)))
+
+
+def ifq_f4_matmul_kernel_name(desc):
+    return _lib().ifq_f4_matmul_kernel_name(ctypes.byref(desc)).decode()
+
+
+def ifq_f4_gated_kernel_name(desc):
+    return _lib().ifq_f4_gated_kernel_name(ctypes.byref(desc)).decode()
+
+
+def ifq_f4_matmul(desc, x, w, w_scales, y, ws=None, stream=None):
+    """ws None: as for ifq_f8_matmul."""
+    d, st = _struct(desc, F4MatmulDesc), _stream(stream)
+    rc = _ffi.call.f4_matmul(d, x, w, w_scales, y, ws, _nbytes(ws), st)
+    if rc == _ffi.IFQ_ERR_INSUFFICIENT_BUFFER and ws is None:
+        ws = _workspace(ifq_f4_matmul_workspace_bytes(desc), y, st)
+        rc = _ffi.call.f4_matmul(d, x, w, w_scales, y, ws, _nbytes(ws), st)
+    if rc:
+        _check(rc, "ifq_f4_matmul")
+
+
+def ifq_f4_gated(desc, x, w_gate, gate_scales, w_up, up_scales, y, ws=None, stream=None):
+    """ws None: as for ifq_f8_matmul."""
+    d, st = _struct(desc, F4MatmulDesc), _stream(stream)
+    rc = _ffi.call.f4_gated(d, x, w_gate, gate_scales, w_up, up_scales, y, ws, _nbytes(ws), st)
+    if rc == _ffi.IFQ_ERR_INSUFFICIENT_BUFFER and ws is None:
+        ws = _workspace(ifq_f4_gated_workspace_bytes(desc), y, st)
+        rc = _ffi.call.f4_gated(d, x, w_gate, gate_scales, w_up, up_scales, y, ws, _nbytes(ws),
+                                st)
+    if rc:
+        _check(rc, "ifq_f4_gated")
+
+
+def ifq_logprobs_workspace_bytes(desc):
+    return int(_lib().ifq_logprobs_workspace_bytes(ctypes.byref(desc)))
+
+
+def ifq_logprobs(desc, logits, tokens, logprob, entropy, top_logprobs, top_tokens, ws=None,
+                 stream=None):
+    """ws None: as for ifq_f8_matmul."""
+    d, st = _struct(desc, LogprobsDesc), _stream(stream)
+    rc = _ffi.call.logprobs(d, logits, tokens, logprob, entropy, top_logprobs, top_tokens, ws,
+                            _nbytes(ws), st)
+    if rc == _ffi.IFQ_ERR_INSUFFICIENT_BUFFER and ws is None:
+        ws = _workspace(ifq_logprobs_workspace_bytes(desc), logits, st)
+        rc = _ffi.call.logprobs(d, logits, tokens, logprob, entropy, top_logprobs, top_tokens,
+                                ws, _nbytes(ws), st)
+    if rc:
+        _check(rc, "ifq_logprobs")

@@ -30,6 +30,11 @@ static struct {
   __typeof__(&ifq_kv_append) kv_append;
   __typeof__(&ifq_kv_read) kv_read;
   __typeof__(&ifq_kv_attention) kv_attention;
+  __typeof__(&ifq_f4_quantize) f4_quantize;
+  __typeof__(&ifq_f4_dequantize) f4_dequantize;
+  __typeof__(&ifq_f4_matmul) f4_matmul;
+  __typeof__(&ifq_f4_gated) f4_gated;
+  __typeof__(&ifq_logprobs) logprobs;
 } fn;
 static PyObject* s_data_ptr;   /* "data_ptr" */
 static PyObject* conv_ptr;     /* the binding's conversion of other tensor arguments */
@@ -120,13 +125,21 @@ ENTRY(kv_append, "pttttttttttp",
 ENTRY(kv_read, "pttttttp", kv_read(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7)))
 ENTRY(kv_attention, "pttttttt" "ip",
       kv_attention(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), (size_t)v[8], P(9)))
+ENTRY(f4_quantize, "ptttp", f4_quantize(P(0), P(1), P(2), P(3), P(4)))
+ENTRY(f4_dequantize, "ptttp", f4_dequantize(P(0), P(1), P(2), P(3), P(4)))
+ENTRY(f4_matmul, "pttttt" "ip",
+      f4_matmul(P(0), P(1), P(2), P(3), P(4), P(5), (size_t)v[6], P(7)))
+ENTRY(f4_gated, "pttttttt" "ip",
+      f4_gated(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), (size_t)v[8], P(9)))
+ENTRY(logprobs, "pttttttt" "ip",
+      logprobs(P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), (size_t)v[8], P(9)))
 
 /* bind(address, integer, addresses in the order of the table above) */
 static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t na) {
-  int64_t v[13];
+  int64_t v[18];
   (void)self;
-  if (na != 15) return PyErr_Format(PyExc_TypeError, "bind: 15 arguments expected");
-  if (values(args + 2, 13, "ppppppppppppp", v)) return NULL;
+  if (na != 20) return PyErr_Format(PyExc_TypeError, "bind: 20 arguments expected");
+  if (values(args + 2, 18, "pppppppppppppppppp", v)) return NULL;
   Py_INCREF(args[0]);
   Py_XSETREF(conv_ptr, args[0]);
   Py_INCREF(args[1]);
@@ -144,6 +157,11 @@ static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t na) {
   fn.kv_append = P(10);
   fn.kv_read = P(11);
   fn.kv_attention = P(12);
+  fn.f4_quantize = P(13);
+  fn.f4_dequantize = P(14);
+  fn.f4_matmul = P(15);
+  fn.f4_gated = P(16);
+  fn.logprobs = P(17);
   Py_RETURN_NONE;
 }
 
@@ -153,6 +171,8 @@ static PyMethodDef methods[] = {M(bind), M(conv_forward), M(conv_forward_fp4),
                                 M(maxpool_codes), M(convert_codes), M(run_stack),
                                 M(run_stack_static), M(f8_quantize), M(f8_matmul),
                                 M(kv_append), M(kv_read), M(kv_attention),
+                                M(f4_quantize), M(f4_dequantize), M(f4_matmul),
+                                M(f4_gated), M(logprobs),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ifqcall", NULL, -1, methods,
                                     NULL, NULL, NULL, NULL};

@@ -124,6 +124,107 @@ ifq_status check_batch(const int32_t* offsets, const int32_t* lengths, const int
   return IFQ_OK;
 }
 
+bool known(int32_t t) { return t == IFQ_TYPE_BF16 || t == IFQ_TYPE_F16 || t == IFQ_TYPE_F32; }
+
+// Bytes of a row of 4-bit codes.
+int64_t code_bytes(int64_t k) { return (k + 31) / 32 * 16; }
+
+ifq_status check_f4_weights(const ifq_f4_weights_desc* d) {
+  if (!d) return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: desc is NULL");
+  if (d->rows < 0 || d->k < 0 || d->rows > kMaxRows || d->k > kMaxRows)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: rows and k must be in 0..2^30");
+  if (!known(d->x_type))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: unknown type %d", d->x_type);
+  if (d->reserved != 0)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: reserved must be 0");
+  if (d->ld_x < d->k || d->ld_codes < code_bytes(d->k) || d->ld_x > kMaxStride ||
+      d->ld_codes > kMaxStride)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: a leading dimension is below its row");
+  if (d->ld_codes % 16)
+    return fail(IFQ_ERR_UNSUPPORTED, "f4 weights: ld_codes must be a multiple of 16");
+  if (ifq::f4_quant_groups(*d) > ifq::kMaxGroups)
+    return fail(IFQ_ERR_UNSUPPORTED, "f4 weights: rows x k is too large for one launch");
+  return IFQ_OK;
+}
+
+ifq_status check_f4_pointers(const ifq_f4_weights_desc* d, const void* x, const void* codes,
+                             const void* scales) {
+  if (!x || !codes || !scales)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: x, codes and scales are required");
+  if (!aligned(x, type_bytes(d->x_type)) || !aligned(codes, 16) || !aligned(scales, 4))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 weights: x must be aligned to its element, codes "
+                "to 16 bytes, scales to 4");
+  return IFQ_OK;
+}
+
+ifq_status check_f4_matmul(const ifq_f4_matmul_desc* d, bool gated) {
+  if (!d) return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: desc is NULL");
+  if (d->m < 0 || d->n < 0 || d->k < 1 || d->m > kMaxRows || d->n > kMaxRows || d->k > kMaxRows)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: need m, n in 0..2^30 and k in 1..2^30");
+  if (d->x_type != IFQ_TYPE_BF16 && d->x_type != IFQ_TYPE_F16)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: x must be bf16 or f16");
+  if (!known(d->y_type))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: unknown type %d", d->y_type);
+  if (gated ? d->activation < IFQ_ACT_SILU || d->activation > IFQ_ACT_GELU_TANH
+            : d->activation != IFQ_ACT_NONE)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, gated ? "f4 gated product: unknown activation %d"
+                                                : "f4 product: activation %d, none expected",
+                d->activation);
+  if (d->reserved != 0)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: reserved must be 0");
+  if (d->ld_x < d->k || d->ld_w < code_bytes(d->k) || d->ld_y < d->n || d->ld_x > kMaxStride ||
+      d->ld_w > kMaxStride || d->ld_y > kMaxStride)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: a leading dimension is below its row");
+  if (d->ld_w % 16)
+    return fail(IFQ_ERR_UNSUPPORTED, "f4 product: ld_w must be a multiple of 16");
+  if (d->ld_w > kMaxProductStride)      // 32-bit offsets within the rows of a tile
+    return fail(IFQ_ERR_UNSUPPORTED, "f4 product: ld_w may be up to 2^25");
+  if (ifq::f4_matmul_groups(*d) > ifq::kMaxGroups)
+    return fail(IFQ_ERR_UNSUPPORTED, "f4 product: m x n is too large for one launch");
+  return IFQ_OK;
+}
+
+ifq_status f4_product(const ifq_f4_matmul_desc* d, bool gated, const void* x, const void* w_gate,
+                      const void* gate_scales, const void* w, const void* w_scales, void* y,
+                      void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (ifq_status st = check_f4_matmul(d, gated)) return st;
+  if (d->m == 0 || d->n == 0) return ifq::set_error(IFQ_OK, "");
+  if (!x || !w || !w_scales || !y || (gated && (!w_gate || !gate_scales)))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: x, the weights, their scales and y are "
+                "required");
+  if (!aligned(x, 2) || !aligned(w, 16) || !aligned(w_gate, 16) || !aligned(w_scales, 4) ||
+      !aligned(gate_scales, 4) || !aligned(y, type_bytes(d->y_type)))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: weights must be 16-byte aligned, scales "
+                "4-byte, x and y to their elements");
+  const size_t need = ifq::f4_matmul_workspace_bytes(*d);
+  if (need && (!ws || ws_bytes < need))
+    return fail(IFQ_ERR_INSUFFICIENT_BUFFER, "f4 product: workspace of %zu bytes, %zu needed",
+                ws ? ws_bytes : (size_t)0, need);
+  if (need && !aligned(ws, 16))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: the workspace must be 16-byte aligned");
+  return launched(ifq::launch_f4_matmul(*d, x, w_gate, gate_scales, w, w_scales, y, ws, stream),
+                  gated ? "f4_gated" : "f4_matmul");
+}
+
+ifq_status check_logprobs(const ifq_logprobs_desc* d) {
+  if (!d) return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: desc is NULL");
+  if (d->rows < 0 || d->n < 1 || d->rows > kMaxRows || d->n > kMaxRows)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: need rows in 0..2^30 and n in 1..2^30");
+  if (!known(d->x_type))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: unknown type %d", d->x_type);
+  if (d->top < 0 || d->top > 64 || d->top > d->n)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: top must be in 0..64 and at most n");
+  if (!(d->scale > 0.0f && d->scale <= 0x1p64f))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: scale must be above 0 and at most 2^64");
+  if (d->reserved != 0)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: reserved must be 0");
+  if (d->ld_x < d->n || d->ld_top < d->top || d->ld_x > kMaxStride || d->ld_top > kMaxStride)
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: a leading dimension is below its row");
+  if (ifq::logprobs_groups(*d) > ifq::kMaxGroups)
+    return fail(IFQ_ERR_UNSUPPORTED, "logprobs: too many rows for one launch");
+  return IFQ_OK;
+}
+
 bool nothing(const ifq_kv_desc* d) { return d->batch == 0 || d->total_q == 0 || d->max_q == 0; }
 
 int64_t head_bytes(const ifq_kv_desc* d) { return (int64_t)d->page_tokens * (d->head_dim + 8); }
@@ -265,6 +366,77 @@ ifq_status ifq_kv_attention(const ifq_kv_desc* d, const void* q, const int32_t* 
     return fail(IFQ_ERR_INVALID_ARGUMENT, "attention: the workspace must be 16-byte aligned");
   return launched(ifq::launch_kv_attention(*d, q, kv_args(d, offsets, lengths, pages, cache),
                                            out, ws, stream), "kv_attention");
+}
+
+ifq_status ifq_f4_quantize(const ifq_f4_weights_desc* d, const void* x, void* codes, void* scales,
+                           hipStream_t stream) {
+  if (ifq_status st = check_f4_weights(d)) return st;
+  if (d->rows == 0 || d->k == 0) return ifq::set_error(IFQ_OK, "");
+  if (ifq_status st = check_f4_pointers(d, x, codes, scales)) return st;
+  return launched(ifq::launch_f4_quantize(*d, x, codes, scales, stream), "f4_quantize");
+}
+
+ifq_status ifq_f4_dequantize(const ifq_f4_weights_desc* d, const void* codes, const void* scales,
+                             void* x, hipStream_t stream) {
+  if (ifq_status st = check_f4_weights(d)) return st;
+  if (d->rows == 0 || d->k == 0) return ifq::set_error(IFQ_OK, "");
+  if (ifq_status st = check_f4_pointers(d, x, codes, scales)) return st;
+  return launched(ifq::launch_f4_dequantize(*d, codes, scales, x, stream), "f4_dequantize");
+}
+
+size_t ifq_f4_matmul_workspace_bytes(const ifq_f4_matmul_desc* d) {
+  return check_f4_matmul(d, false) ? 0 : ifq::f4_matmul_workspace_bytes(*d);
+}
+
+size_t ifq_f4_gated_workspace_bytes(const ifq_f4_matmul_desc* d) {
+  return check_f4_matmul(d, true) ? 0 : ifq::f4_matmul_workspace_bytes(*d);
+}
+
+const char* ifq_f4_matmul_kernel_name(const ifq_f4_matmul_desc* d) {
+  return check_f4_matmul(d, false) ? "" : ifq::f4_matmul_kernel_name(*d);
+}
+
+const char* ifq_f4_gated_kernel_name(const ifq_f4_matmul_desc* d) {
+  return check_f4_matmul(d, true) ? "" : ifq::f4_matmul_kernel_name(*d);
+}
+
+ifq_status ifq_f4_matmul(const ifq_f4_matmul_desc* d, const void* x, const void* w,
+                         const void* w_scales, void* y, void* ws, size_t ws_bytes,
+                         hipStream_t stream) {
+  return f4_product(d, false, x, nullptr, nullptr, w, w_scales, y, ws, ws_bytes, stream);
+}
+
+ifq_status ifq_f4_gated(const ifq_f4_matmul_desc* d, const void* x, const void* w_gate,
+                        const void* gate_scales, const void* w_up, const void* up_scales,
+                        void* y, void* ws, size_t ws_bytes, hipStream_t stream) {
+  return f4_product(d, true, x, w_gate, gate_scales, w_up, up_scales, y, ws, ws_bytes, stream);
+}
+
+size_t ifq_logprobs_workspace_bytes(const ifq_logprobs_desc* d) {
+  return check_logprobs(d) ? 0 : ifq::logprobs_workspace_bytes(*d);
+}
+
+ifq_status ifq_logprobs(const ifq_logprobs_desc* d, const void* logits, const int32_t* tokens,
+                        float* logprob, float* entropy, float* top_logprobs, int32_t* top_tokens,
+                        void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (ifq_status st = check_logprobs(d)) return st;
+  if (d->rows == 0) return ifq::set_error(IFQ_OK, "");
+  if (!logits || (tokens == nullptr) != (logprob == nullptr))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: logits are required, logprob goes with "
+                "tokens");
+  if ((d->top > 0) != (top_logprobs != nullptr) || (d->top > 0) != (top_tokens != nullptr))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: top_logprobs and top_tokens go with top > 0");
+  if (!aligned(logits, type_bytes(d->x_type)) || !aligned(tokens, 4) || !aligned(logprob, 4) ||
+      !aligned(entropy, 4) || !aligned(top_logprobs, 4) || !aligned(top_tokens, 4))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: arrays must be aligned to their elements");
+  const size_t need = ifq::logprobs_workspace_bytes(*d);
+  if (need && (!ws || ws_bytes < need))
+    return fail(IFQ_ERR_INSUFFICIENT_BUFFER, "logprobs: workspace of %zu bytes, %zu needed",
+                ws ? ws_bytes : (size_t)0, need);
+  if (need && !aligned(ws, 16))
+    return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: the workspace must be 16-byte aligned");
+  return launched(ifq::launch_logprobs(*d, logits, tokens, logprob, entropy, top_logprobs,
+                                       top_tokens, ws, stream), "logprobs");
 }
 
 }  // extern "C"

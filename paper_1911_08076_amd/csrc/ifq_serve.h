@@ -1,7 +1,8 @@
 // Internals of the operators for serving language models: the 8-bit float
 // quantizer and block-scaled product (ifq_f8.hip), the paged cache of 4-bit
-// codes (ifq_kv.hip) and attention over it (ifq_attn.hip). Arguments reach the
-// launchers validated (ifq_serve.cpp).
+// codes (ifq_kv.hip) and attention over it (ifq_attn.hip), weights in 4-bit floats
+// and the products with them (ifq_f4.hip), log probabilities (ifq_logprobs.hip).
+// Arguments reach the launchers validated (ifq_serve.cpp).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -44,6 +45,26 @@ size_t kv_attention_workspace_bytes(const ifq_kv_desc& d);
 const char* kv_attention_kernel_name(const ifq_kv_desc& d);
 hipError_t launch_kv_attention(const ifq_kv_desc& d, const void* q, const KvArgs& a, void* out,
                                void* ws, hipStream_t stream);
+
+int64_t f4_quant_groups(const ifq_f4_weights_desc& d);   // workgroups of its launches
+hipError_t launch_f4_quantize(const ifq_f4_weights_desc& d, const void* x, void* codes,
+                              void* scales, hipStream_t stream);
+hipError_t launch_f4_dequantize(const ifq_f4_weights_desc& d, const void* codes,
+                                const void* scales, void* x, hipStream_t stream);
+
+// The product, and with an activation the gated one (w_gate is unused without).
+size_t f4_matmul_workspace_bytes(const ifq_f4_matmul_desc& d);
+int64_t f4_matmul_groups(const ifq_f4_matmul_desc& d);
+const char* f4_matmul_kernel_name(const ifq_f4_matmul_desc& d);
+hipError_t launch_f4_matmul(const ifq_f4_matmul_desc& d, const void* x, const void* w_gate,
+                            const void* gate_scales, const void* w, const void* w_scales,
+                            void* y, void* ws, hipStream_t stream);
+
+size_t logprobs_workspace_bytes(const ifq_logprobs_desc& d);
+int64_t logprobs_groups(const ifq_logprobs_desc& d);
+hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const int32_t* tokens,
+                           float* logprob, float* entropy, float* top_logprobs,
+                           int32_t* top_tokens, void* ws, hipStream_t stream);
 
 #ifdef __HIPCC__
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -1,0 +1,182 @@
+"""Log probabilities of given tokens, entropy and top tokens on the GPU, within the
+oracle's bounds for fp32; tokens must be equal."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1911_08076_amd as P
+from oracle import logprobs as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": (torch.bfloat16, P.IFQ_TYPE_BF16), "f16": (torch.float16, P.IFQ_TYPE_F16),
+         "f32": (torch.float32, P.IFQ_TYPE_F32)}
+
+
+def call(x, tokens, top, scale, ld_x=None, ld_top=None, ws=None, kind=None, rows=None, n=None):
+    rows, n = (x.shape if rows is None else (rows, n))
+    kind = {v[0]: v[1] for v in TYPES.values()}[x.dtype] if kind is None else kind
+    d = P.logprobs_desc(rows, n, kind, top, scale, ld_x, ld_top)
+    lp, h = (torch.full((rows + 1,), -77.0, device=DEV) for _ in range(2))
+    best = torch.full((rows, ld_top or top), -77.0, device=DEV) if top else None
+    at = torch.full((rows, ld_top or top), -77, dtype=torch.int32, device=DEV) if top else None
+    P.ifq_logprobs(d, x, tokens, lp, h, best, at, ws=ws)
+    assert lp[rows] == -77 and h[rows] == -77
+    if top:
+        assert (best[:, top:] == -77).all() and (at[:, top:] == -77).all()
+        best, at = best[:, :top].cpu().numpy(), at[:, :top].cpu().numpy()
+    return lp[:rows].cpu().numpy(), h[:rows].cpu().numpy(), best, at
+
+
+def within(got, want, bound):
+    # what is half a step or more past fp32's largest number, 2^128 - 2^104, is infinite in it
+    want = np.where(np.abs(want) >= 2.0 ** 128 - 2.0 ** 103, np.copysign(np.inf, want), want)
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    with np.errstate(invalid="ignore"):
+        off = np.where(same, 0.0, np.abs(got - want))
+        # and the rounding to fp32 of what is returned
+        assert (off <= bound + 2.0 ** -24 * np.where(same, 0.0, np.abs(want))).all(), (
+            np.nanmax(off / np.maximum(bound, 1e-30)))
+
+
+def check(x, tokens, top=0, scale=1.0, **more):
+    """x: device logits; tokens: a list."""
+    got = call(x, torch.tensor(tokens, dtype=torch.int32, device=DEV), top, scale, **more)
+    (lp, h, best, at), (blp, bh, bbest) = O.logprobs(x.double().cpu().numpy(), tokens, top,
+                                                    float(np.float32(scale)))
+    within(got[0], lp, blp)
+    within(got[1], h, bh)
+    if top:
+        assert np.array_equal(got[3], at)
+        within(got[2], best, bbest)
+
+
+def logits(rng, rows, n, kind, spread=3.0):
+    x = rng.standard_normal((rows, n)) * spread
+    return torch.from_numpy(x).to(TYPES[kind][0]).to(DEV)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,n,top", [
+    (1, 1, 1), (1, 1, 0), (2, 2, 2), (3, 5, 3), (1, 63, 63), (4, 64, 64), (3, 65, 64), (5, 777, 5),
+    (2, 2048, 20), (3, 2049, 20), (2, 8191, 64), (3, 8193, 1), (1, 16385, 33), (2, 50001, 5),
+    (1, 128000, 20), (40, 9001, 7), (700, 3000, 3), (2, 300000, 64)])
+def test_logprobs(kind, rows, n, top, rng):
+    tokens = rng.integers(0, n, rows).tolist()
+    check(logits(rng, rows, n, kind), tokens, top)
+    check(logits(rng, rows, n, kind), tokens, top, scale=0.7)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_logprobs_many_rows(kind, rng):
+    check(logits(rng, 3000, 401, kind), rng.integers(0, 401, 3000).tolist(), 4)
+
+
+@pytest.mark.parametrize("n", [100, 3000, 40000])
+@pytest.mark.parametrize("top", [0, 9])
+def test_logprobs_outputs_left_out(n, top, rng):
+    x = logits(rng, 3, n, "f32")
+    tokens = torch.tensor([1, 2, 3], dtype=torch.int32, device=DEV)
+    want = call(x, tokens, top, 1.0)
+    d = P.logprobs_desc(3, n, P.IFQ_TYPE_F32, top)
+    best = torch.empty(3, top, device=DEV) if top else None
+    at = torch.empty(3, top, dtype=torch.int32, device=DEV) if top else None
+    lp, h = torch.empty(3, device=DEV), torch.empty(3, device=DEV)
+    P.ifq_logprobs(d, x, tokens, lp, None, best, at)
+    P.ifq_logprobs(d, x, None, None, h, best, at)
+    assert np.array_equal(lp.cpu().numpy(), want[0]) and np.array_equal(h.cpu().numpy(), want[1])
+    if top:
+        assert np.array_equal(at.cpu().numpy(), want[3])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n", [90, 5000, 70000])
+def test_logprobs_masks(kind, n, rng):
+    """Infinities, the type's lowest value, rows in which nothing or one thing is left."""
+    low = torch.finfo(TYPES[kind][0]).min
+    x = logits(rng, 14, n, kind)
+    hide = torch.from_numpy(rng.random((14, n)) < 0.9).to(DEV)
+    x[0][hide[0]] = -np.inf
+    x[1][hide[1]] = low
+    x[2] = -np.inf
+    x[3] = low
+    x[4] = -np.inf
+    x[4, n // 2] = -5.0
+    x[5] = low
+    x[5, n - 1] = 3.0
+    x[6, n // 3] = np.nan
+    x[7, n - 1] = np.inf
+    x[8] = 0.0
+    x[9, ::2] = -0.0
+    x[9, 1::2] = 0.0
+    x[10] = np.nan
+    x[11] = np.inf
+    x[12] = -np.inf
+    x[12, 3] = low
+    x[13, 0] = -torch.finfo(TYPES[kind][0]).max
+    x[13, 1] = torch.finfo(TYPES[kind][0]).max
+    tokens = [n // 2] * 14
+    tokens[5], tokens[12], tokens[13] = 0, 3, 0
+    check(x, tokens, 20)
+    check(x, tokens, 0, scale=3.0)
+    check(x, [-1, n, -5, 0, n - 1, 1, -1, n, 0, 1, -1, -1, 2 ** 31 - 1, -2 ** 31], 20, scale=0.01)
+
+
+@pytest.mark.parametrize("n", [64, 2500, 33000])
+def test_logprobs_orders(n, rng):
+    """Rising, falling and tied values, the best at either end, ties across lanes and parts."""
+    x = torch.empty(8, n, device=DEV)
+    ramp = torch.arange(n, device=DEV) * 1e-3
+    x[0], x[1] = ramp, -ramp
+    x[2] = torch.arange(n, device=DEV) % 7
+    x[3] = 1.0
+    x[4] = 0.0
+    x[4, -10:] = 5.0
+    x[5] = torch.arange(n, device=DEV) // 50
+    x[6] = -(torch.arange(n, device=DEV) // 50)
+    x[7] = torch.from_numpy(rng.integers(0, 5, n)).to(x)
+    for kind in TYPES:
+        for top in (1, 20, 64):
+            check(x.to(TYPES[kind][0]), [n - 1] * 8, top)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-3, 100.0, 2.0 ** 64])
+def test_logprobs_temperatures(scale, rng):
+    check(logits(rng, 4, 3000, "f32"), [1, 2, 3, 4], 5, scale=scale)
+    check(logits(rng, 1, 50000, "bf16"), [7], 5, scale=scale)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", [(4, 601), (2, 30001)])
+def test_logprobs_strides(kind, rows, n, rng):
+    """Rows that begin at any element, NaN around them, and wider rows of outputs."""
+    ld = n + 6
+    held = torch.full((rows * ld + 3,), np.nan, dtype=TYPES[kind][0], device=DEV)
+    for offset in (0, 1, 3):
+        view = held[offset:offset + rows * ld].view(rows, ld)
+        x = logits(rng, rows, n, kind)
+        view[:, :n] = x
+        tokens = rng.integers(0, n, rows).tolist()
+        got = call(held[offset:], torch.tensor(tokens, dtype=torch.int32, device=DEV), 6, 1.0,
+                   ld_x=ld, ld_top=9, kind=TYPES[kind][1], rows=rows, n=n)
+        want = call(x, torch.tensor(tokens, dtype=torch.int32, device=DEV), 6, 1.0)
+        assert all(np.array_equal(a, b) for a, b in zip(got, want))
+        view[:] = np.nan
+
+
+def test_logprobs_same_bits_on_a_shared_workspace(rng):
+    """One workspace for calls of several sizes, as one program keeps it; parts in any order."""
+    sizes = [(1, 128000, 20), (7, 33000, 64), (3, 50001, 0)]
+    kept = []
+    need = max(P.ifq_logprobs_workspace_bytes(P.logprobs_desc(r, n, P.IFQ_TYPE_F32, t))
+               for r, n, t in sizes)
+    assert need
+    ws = torch.zeros(need, dtype=torch.uint8, device=DEV)
+    for r, n, t in sizes:
+        x = logits(rng, r, n, "f32")
+        kept.append((x, torch.zeros(r, dtype=torch.int32, device=DEV), t))
+    first = [call(x, k, t, 1.0) for x, k, t in kept]
+    for _ in range(5):
+        for (x, k, t), want in zip(kept, first):
+            got = call(x, k, t, 1.0, ws=ws)
+            assert all(b is None or np.array_equal(a, b) for a, b in zip(got, want))
