@@ -10,6 +10,8 @@
 namespace ifq {
 namespace {
 
+typedef float v16f __attribute__((ext_vector_type(16)));
+
 // Columns whose four scales lie together: a row's 64 bytes of codes.
 constexpr int kF4Block = 128;
 
@@ -157,7 +159,8 @@ struct F4MatmulArgs {
   int64_t ld_x, ld_w, ld_y;
   int32_t m, n, k, kb;
   int32_t y_type, activation;
-  int32_t groups_n;              // workgroups along n
+  int32_t groups_n;              // few rows: workgroups along n
+  int32_t groups_m;              // tiles: workgroups along m
 };
 
 template <typename T> struct Half;
@@ -169,6 +172,9 @@ template <> struct Half<__bf16> {
   static __device__ __forceinline__ f32x4 mma16(x8 a, x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ v16f mma32(x8 a, x8 b, v16f c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
 };
 template <> struct Half<_Float16> {
   typedef f16x8 x8;
@@ -177,6 +183,9 @@ template <> struct Half<_Float16> {
   }
   static __device__ __forceinline__ f32x4 mma16(x8 a, x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ v16f mma32(x8 a, x8 b, v16f c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
 };
 
@@ -300,13 +309,275 @@ __global__ __launch_bounds__(64 * KS) void f4_matmul_few(F4MatmulArgs a) {
   }
 }
 
-int64_t groups_of(int64_t m, int64_t n) { return (m + 31) / 32 * ((n + 15) / 16); }
+// Sixteen zero bytes: what loads past the end of a row of x read.
+__device__ const u32x4 g_zero = {0, 0, 0, 0};
+
+// 16 bytes per lane straight into LDS at dst (uniform) + 16 * lane: from a
+// pointer per lane, or from a uniform base and an offset per lane. The waits
+// for them are the caller's. A load into LDS must not follow the write of M0
+// directly: one wait state, which the compiler does not add inside asm.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_lds16(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(dst), "v"(src) : "memory", "m0");
+}
+__device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(dst), "v"(off), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// A wave-uniform pointer that the compiler cannot tell for one.
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t*>((uintptr_t)((uint64_t)hi << 32 | lo));
+}
+
+// Many activation rows: a workgroup takes 32 * MT of them, in LDS, and its WN
+// waves 32 * NT weight rows each, which go from memory to registers, so that a code
+// is converted once in the workgroup. Rows of x lie in LDS as 256 bytes a block of
+// 128 columns, in 16-byte cells of which row r holds cell c at place c ^ (r & 15): the
+// 16 rows of which a read takes a cell each at a time then spread over all 64
+// banks. A lane of half h takes the groups 2 h and 2 h + 1 of its weight rows, and cells
+// 8 h + 4 j + i of its activation rows beside word i of group 2 h + j.
+//
+// DIRECT: x goes from memory into LDS, two blocks in turn; it needs 16-byte aligned
+// rows of whole cells. Otherwise it goes through registers.
+template <typename T, int MT, int NT, int WN, int WK, int HALVES, bool DIRECT>
+__global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs a) {
+  constexpr int TM = 32 * MT, ROWS = TM / WN, LOADS = ROWS / 4;
+  constexpr int TN = 32 * NT / HALVES;          // columns of y for a wave
+  static_assert(TM % (4 * WN) == 0 && NT % HALVES == 0, "");
+  __shared__ __align__(16) uint8_t lds[WK][2][TM][256];
+  const int any = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = any % WN, half = any / WN;
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  // tiles that follow one another on an XCD share their weight rows
+  const int each = (gridDim.x + 7) / 8, over = gridDim.x & 7;
+  const int xcd = blockIdx.x & 7;
+  const int tile = (over == 0 || xcd < over ? xcd * each : over * each + (xcd - over) * (each - 1)) +
+                   (blockIdx.x >> 3);
+  const int m0 = tile % a.groups_m * TM, n0 = tile / a.groups_m * (WN * TN) + wave * TN;
+
+  const uint8_t* wp[NT];
+  const uint8_t* sp[NT];
+#pragma unroll
+  for (int z = 0; z < NT; ++z) {
+    const int n = min(n0 + 32 * (z / HALVES) + r, a.n - 1), from = HALVES == 2 ? z % 2 : 1;
+    wp[z] = a.w[from] + n * a.ld_w + 32 * h;
+    sp[z] = a.s[from] + (int64_t)n * 4 + 2 * h;
+  }
+  const int64_t sstep = (int64_t)a.n * 4;
+  // this wave's rows of x
+  const int x0 = min(m0 + ROWS * wave, a.m - 1);
+  const uint8_t* xbase = uniform(static_cast<const uint8_t*>(a.x) + x0 * a.ld_x * 2);
+  uint32_t xoff[LOADS];
+  int cell[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int row = 4 * i + (lane >> 4);
+    cell[i] = (lane & 15) ^ ((ROWS * wave + row) & 15);
+    xoff[i] = DIRECT ? (uint32_t)(min(row, a.m - 1 - x0) * (int32_t)a.ld_x * 2) + 16 * cell[i] : 0;
+  }
+  const uint32_t to0 =
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[half][0][0][0] +
+      ROWS * wave * 256;
+  typename Half<T>::x8 held[DIRECT ? 1 : LOADS];
+  auto load_x = [&](int b, int turn) {
+    if constexpr (DIRECT) {
+      const uint32_t to = to0 + turn * TM * 256;
+      const uint8_t* base = xbase + (int64_t)b * 256;
+      if ((b + 1) * kF4Block <= a.k) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_lds16(base, xoff[i], to + 1024 * i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          load_lds16(b * kF4Block + 8 * cell[i] < a.k ? (const void*)(base + xoff[i]) : &g_zero,
+                     to + 1024 * i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int64_t row = min(x0 + 4 * i + (lane >> 4), a.m - 1);
+        held[i] = load_x8(static_cast<const T*>(a.x) + row * a.ld_x, b * kF4Block + 8 * cell[i],
+                          a.k);
+      }
+    }
+  };
+  auto store_x = [&](int turn) {
+    if constexpr (!DIRECT)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        *reinterpret_cast<typename Half<T>::x8*>(
+            &lds[half][turn][ROWS * wave + 4 * i + (lane >> 4)][16 * (lane & 15)]) = held[i];
+  };
+  u32x4 next[NT][2];
+  uint32_t next_s[NT];
+  auto load_w = [&](int b) {
+    const bool whole = (b + 1) * kF4Block <= a.k;
+#pragma unroll
+    for (int z = 0; z < NT; ++z) {
+      const uint8_t* p = wp[z] + (int64_t)b * 64;
+      next_s[z] = *reinterpret_cast<const uint16_t*>(sp[z] + b * sstep);
+      if (whole) {
+        next[z][0] = *reinterpret_cast<const u32x4*>(p);
+        next[z][1] = *reinterpret_cast<const u32x4*>(p + 16);
+      } else {
+        // groups past k: no codes, and not their scale
+        const int c = b * kF4Block + 64 * h;
+        next[z][0] = next[z][1] = u32x4{0, 0, 0, 0};
+        if (c < a.k) next[z][0] = *reinterpret_cast<const u32x4*>(p);
+        if (c + 32 < a.k) next[z][1] = *reinterpret_cast<const u32x4*>(p + 16);
+        next_s[z] &= c + 32 < a.k ? 0xFFFFu : c < a.k ? 0xFFu : 0u;
+      }
+    }
+  };
+  v16f acc[MT][NT];
+#pragma unroll
+  for (int x = 0; x < MT; ++x)
+#pragma unroll
+    for (int z = 0; z < NT; ++z) acc[x][z] = v16f{};
+  if (half < a.kb) {
+    load_x(half, 0);
+    load_w(half);
+    store_x(0);
+  }
+  int turn = 0;
+  for (int b = half; b < a.kb + half; b += WK, turn ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (WK > 1 && b >= a.kb) break;              // the last wait of a half with a block less
+    // taken before the next loads: the compiler's wait for these costs nothing here, and
+    // later would count the loads into LDS
+    u32x4 codes[NT][2];
+    uint32_t scales[NT];
+#pragma unroll
+    for (int z = 0; z < NT; ++z) {
+      codes[z][0] = next[z][0];
+      codes[z][1] = next[z][1];
+      scales[z] = next_s[z];
+      asm volatile("" : "+v"(codes[z][0]), "+v"(codes[z][1]), "+v"(scales[z]));
+    }
+    const bool more = b + WK < a.kb;
+    if (more) {
+      load_x(b + WK, turn ^ 1);
+      load_w(b + WK);
+    }
+    const uint8_t(*at)[256] = lds[half][turn];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        typename Half<T>::x8 xv[MT], wv[NT];
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+          xv[x] = *reinterpret_cast<const typename Half<T>::x8*>(
+              &at[32 * x + r][16 * ((8 * h + 4 * j + i) ^ (r & 15))]);
+#pragma unroll
+        for (int z = 0; z < NT; ++z)
+          wv[z] = operand<T>(codes[z][j][i], f4_scale(scales[z] >> (8 * j) & 255u));
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+#pragma unroll
+          for (int z = 0; z < NT; ++z) acc[x][z] = Half<T>::mma32(wv[z], xv[x], acc[x][z]);
+      }
+    if (more) store_x(turn ^ 1);
+  }
+  if constexpr (WK > 1) {
+    static_assert(WK == 2 && sizeof(lds) >= sizeof(float) * 64 * WN * MT * NT * 16, "");
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(&lds[0][0][0][0]) + threadIdx.x % (64 * WN);
+    if (half) {
+#pragma unroll
+      for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int z = 0; z < NT; ++z)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sums[((x * NT + z) * 16 + e) * 64 * WN] = acc[x][z][e];
+    }
+    __syncthreads();
+    if (half) return;
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+      for (int z = 0; z < NT; ++z)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[x][z][e] += sums[((x * NT + z) * 16 + e) * 64 * WN];
+  }
+#pragma unroll
+  for (int x = 0; x < MT; ++x) {
+    const int m = m0 + 32 * x + r;
+    if (m >= a.m) continue;
+#pragma unroll
+    for (int z = 0; z < NT; z += HALVES)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = n0 + 32 * (z / HALVES) + 8 * e + 4 * h;
+        if (n >= a.n) continue;
+        f32x4 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v[q] = acc[x][z][4 * e + q];
+          if (HALVES == 2) v[q] = activate(v[q], a.activation) * acc[x][z + HALVES - 1][4 * e + q];
+        }
+        store4(a.y, a.y_type, m * a.ld_y + n, v, a.n - n);
+      }
+  }
+}
+
+int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+enum Way { kRows, kTiles };
+
+struct Plan {
+  Way way;
+  int32_t halves;    // tiles: groups of waves that share k
+  int64_t groups;    // workgroups
+};
+
+Plan plan_of(const ifq_f4_matmul_desc& d) {
+  const int each = d.activation ? 128 : 256;       // columns of y for a tile
+  Plan p = {d.m > 64 ? kTiles : kRows, 1, 0};
+  if (p.way == kRows) {
+    p.groups = ceil_of(d.m, 32) * ceil_of(d.n, 16);
+  } else {
+    p.groups = ceil_of(d.m, 128) * ceil_of(d.n, each);
+    if (p.groups <= 256 && d.k >= 1024) p.halves = 2;
+  }
+  return p;
+}
 
 template <typename T, int HALVES>
-void few(F4MatmulArgs& a, hipStream_t stream) {
+void few(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
   a.groups_n = (a.n + 15) / 16;
-  const dim3 grid((uint32_t)groups_of(a.m, a.n)), block(256);
+  const dim3 grid((uint32_t)p.groups), block(256);
   hipLaunchKernelGGL((f4_matmul_few<T, 2, 4, HALVES>), grid, block, 0, stream, a);
+}
+
+template <typename T, int HALVES, bool DIRECT>
+void tiled(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
+  a.groups_m = (a.m + 127) / 128;
+  const dim3 grid((uint32_t)p.groups);
+  if (p.halves == 2)
+    hipLaunchKernelGGL((f4_matmul_tiled<T, 4, 2, 4, 2, HALVES, DIRECT>), grid, dim3(512), 0,
+                       stream, a);
+  else
+    hipLaunchKernelGGL((f4_matmul_tiled<T, 4, 2, 4, 1, HALVES, DIRECT>), grid, dim3(256), 0,
+                       stream, a);
+}
+
+template <typename T, int HALVES>
+void matmul(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
+  if (p.way == kRows) return few<T, HALVES>(a, p, stream);
+  // whole cells of 16 bytes, and 32-bit offsets within the rows of a tile
+  const bool direct = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.ld_x % 8 == 0 &&
+                      a.k % 8 == 0 && a.ld_x <= (1 << 22);
+  if (direct) tiled<T, HALVES, true>(a, p, stream);
+  else tiled<T, HALVES, false>(a, p, stream);
 }
 
 F4QuantArgs quant_args(const ifq_f4_weights_desc& d, const void* codes, const void* scales) {
@@ -366,12 +637,16 @@ hipError_t launch_f4_dequantize(const ifq_f4_weights_desc& d, const void* codes,
 size_t f4_matmul_workspace_bytes(const ifq_f4_matmul_desc&) { return 0; }
 
 int64_t f4_matmul_groups(const ifq_f4_matmul_desc& d) {
-  return d.m == 0 || d.n == 0 ? 0 : groups_of(d.m, d.n);
+  return d.m == 0 || d.n == 0 ? 0 : plan_of(d).groups;
 }
 
 const char* f4_matmul_kernel_name(const ifq_f4_matmul_desc& d) {
   if (d.m == 0 || d.n == 0) return "";
-  return d.activation ? "f4_matmul_few<2, 4, 2>" : "f4_matmul_few<2, 4, 1>";
+  const Plan p = plan_of(d);
+  if (p.way == kRows) return d.activation ? "f4_matmul_few<2, 4, 2>" : "f4_matmul_few<2, 4, 1>";
+  if (p.halves == 2)
+    return d.activation ? "f4_matmul_tiled<4, 2, 4, 2, 2>" : "f4_matmul_tiled<4, 2, 4, 2, 1>";
+  return d.activation ? "f4_matmul_tiled<4, 2, 4, 1, 2>" : "f4_matmul_tiled<4, 2, 4, 1, 1>";
 }
 
 hipError_t launch_f4_matmul(const ifq_f4_matmul_desc& d, const void* x, const void* w_gate,
@@ -393,12 +668,13 @@ hipError_t launch_f4_matmul(const ifq_f4_matmul_desc& d, const void* x, const vo
   a.kb = (int32_t)((d.k + kF4Block - 1) / kF4Block);
   a.y_type = d.y_type;
   a.activation = d.activation;
+  const Plan p = plan_of(d);
   if (d.x_type == IFQ_TYPE_BF16) {
-    if (d.activation) few<__bf16, 2>(a, stream);
-    else few<__bf16, 1>(a, stream);
+    if (d.activation) matmul<__bf16, 2>(a, p, stream);
+    else matmul<__bf16, 1>(a, p, stream);
   } else {
-    if (d.activation) few<_Float16, 2>(a, stream);
-    else few<_Float16, 1>(a, stream);
+    if (d.activation) matmul<_Float16, 2>(a, p, stream);
+    else matmul<_Float16, 1>(a, p, stream);
   }
   return hipGetLastError();
 }
