@@ -240,77 +240,13 @@ __device__ __forceinline__ typename Half<T>::x8 load_x8(const T* row, int c, int
   return v;
 }
 
-// Few activation rows. A workgroup takes 16 weight rows (of each half, where
-// HALVES is 2) and 16 * MT activation rows, its KS waves every KS-th block of 128
-// columns; the waves' sums are added in LDS in their order.
-template <typename T, int MT, int KS, int HALVES>
-__global__ __launch_bounds__(64 * KS) void f4_matmul_few(F4MatmulArgs a) {
-  __shared__ __align__(16) float sums[KS][HALVES][MT][64][4];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x % a.groups_n * 16, m0 = blockIdx.x / a.groups_n * 16 * MT;
-  const int wrow = min(n0 + r, a.n - 1);
-  const T* xrow[MT];
-#pragma unroll
-  for (int x = 0; x < MT; ++x)
-    xrow[x] = static_cast<const T*>(a.x) + (int64_t)min(m0 + 16 * x + r, a.m - 1) * a.ld_x;
-  f32x4 acc[HALVES][MT];
-#pragma unroll
-  for (int z = 0; z < HALVES; ++z)
-#pragma unroll
-    for (int x = 0; x < MT; ++x) acc[z][x] = f32x4{0, 0, 0, 0};
-  for (int b = wave; b < a.kb; b += KS) {
-    const int c = b * kF4Block + 32 * g;
-    u32x4 codes[HALVES];
-    float scale[HALVES];
-#pragma unroll
-    for (int z = 0; z < HALVES; ++z) {
-      const int from = z + 2 - HALVES;
-      codes[z] = u32x4{0, 0, 0, 0};
-      scale[z] = 0.0f;                       // a group past k, whatever its byte
-      if (c < a.k) {
-        codes[z] = *reinterpret_cast<const u32x4*>(a.w[from] + wrow * a.ld_w + c / 2);
-        scale[z] = f4_scale(a.s[from][((int64_t)b * a.n + wrow) * 4 + g]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      typename Half<T>::x8 xv[MT];
-#pragma unroll
-      for (int x = 0; x < MT; ++x) xv[x] = load_x8(xrow[x], c + 8 * i, a.k);
-#pragma unroll
-      for (int z = 0; z < HALVES; ++z) {
-        const auto wv = operand<T>(codes[z][i], scale[z]);
-#pragma unroll
-        for (int x = 0; x < MT; ++x) acc[z][x] = Half<T>::mma16(wv, xv[x], acc[z][x]);
-      }
-    }
-  }
-#pragma unroll
-  for (int z = 0; z < HALVES; ++z)
-#pragma unroll
-    for (int x = 0; x < MT; ++x) *reinterpret_cast<f32x4*>(sums[wave][z][x][lane]) = acc[z][x];
-  __syncthreads();
-  for (int i = threadIdx.x; i < 64 * MT; i += 64 * KS) {
-    const int x = i >> 6, l = i & 63, n = n0 + 4 * (l >> 4), m = m0 + 16 * x + (l & 15);
-    f32x4 v[HALVES];
-#pragma unroll
-    for (int z = 0; z < HALVES; ++z) {
-      v[z] = *reinterpret_cast<const f32x4*>(sums[0][z][x][l]);
-#pragma unroll
-      for (int w = 1; w < KS; ++w) v[z] += *reinterpret_cast<const f32x4*>(sums[w][z][x][l]);
-    }
-    if (m < a.m && n < a.n) {
-      if constexpr (HALVES == 2)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[0][e] = activate(v[0][e], a.activation) * v[1][e];
-      store4(a.y, a.y_type, (int64_t)m * a.ld_y + n, v[0], a.n - n);
-    }
-  }
-}
+// Stages of LDS of a wave of few rows: weights, scales, x; and how many there are.
+constexpr int few_stage(int xr, int nt) { return 1024 * nt + 256 + 256 * xr; }
+constexpr int few_ahead(int xr) { return xr <= 8 ? 4 : xr <= 16 ? 3 : 2; }
+constexpr int kLdsBytes = 160 * 1024;
 
-// Sixteen zero bytes: what loads past the end of a row of x read.
-__device__ const u32x4 g_zero = {0, 0, 0, 0};
+// Zeros: what loads past the end of a row read.
+__device__ const u32x4 g_zero[1] = {};
 
 // 16 bytes per lane straight into LDS at dst (uniform) + 16 * lane: from a
 // pointer per lane, or from a uniform base and an offset per lane. The waits
@@ -326,7 +262,22 @@ __device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t off, ui
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(dst), "v"(off), "s"(base) : "memory", "m0");
 }
+__device__ __forceinline__ void load_lds4(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :: "s"(dst), "v"(src) : "memory", "m0");
+}
 #pragma clang diagnostic pop
+
+// Waits until no more than `left` groups of LOADS loads are on their way.
+template <int LOADS, int MOST>
+__device__ __forceinline__ void wait_loads(int left) {
+  if constexpr (MOST == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    if (left >= MOST) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS * MOST) : "memory");
+    else wait_loads<LOADS, MOST - 1>(left);
+  }
+}
 
 // A wave-uniform pointer that the compiler cannot tell for one.
 __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
@@ -334,6 +285,154 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
   return reinterpret_cast<const uint8_t*>((uintptr_t)((uint64_t)hi << 32 | lo));
+}
+
+// Few activation rows. A workgroup takes 16 * NT weight rows (of both halves
+// together, where HALVES is 2) and XR activation rows, its waves every so many-th
+// block of 128 columns; the waves' sums are added in LDS in their order.
+//
+// A wave brings its blocks through LDS of its own, AHEAD of them on their way at a time:
+// there consecutive lanes read consecutive 16 bytes of a row, 64 of weights and 256
+// of x, where the operands' own order (16 lanes in 16 rows) takes a cycle for each lane
+// (7 x 128000 x 4096 102 us, 32 x 4096 x 14336 34). Rows of weights lie 64 bytes
+// apart with group c at place c ^ (r / 4 & 3), rows of x 256 with cell c at c ^ (r & 15):
+// the 16 rows of which a read takes 16 bytes each at a time spread over all 64 banks.
+//
+// DIRECT: x goes from memory into LDS; it needs 16-byte aligned rows of whole cells.
+// Otherwise it goes through registers, a block ahead.
+template <typename T, int XR, int NT, int HALVES, bool DIRECT>
+__global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
+  constexpr int MT = (XR + 15) / 16, COLUMNS = 16 * NT / HALVES;
+  constexpr int AHEAD = few_ahead(XR), STAGE = few_stage(XR, NT);
+  constexpr int LOADS = NT + 1 + (DIRECT ? XR / 4 : 0);
+  extern __shared__ __align__(16) uint8_t few_lds[];        // [wave][AHEAD][STAGE], then sums
+  typedef typename Half<T>::x8 x8;
+  const int waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x % a.groups_n * COLUMNS, m0 = blockIdx.x / a.groups_n * XR;
+  uint8_t* const own = few_lds + wave * (AHEAD * STAGE);
+  const uint32_t to0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)own;
+  // what this lane loads: group `piece` of row lane / 4, scales of row lane, and
+  // cell `cell` of rows 4 i + lane / 16
+  const int piece = (lane & 3) ^ (lane >> 4 & 3);
+  const uint8_t* wp[NT];
+#pragma unroll
+  for (int z = 0; z < NT; ++z) {
+    const int n = min(n0 + 16 * (z / HALVES) + (lane >> 2), a.n - 1);
+    wp[z] = a.w[HALVES == 2 ? z % 2 : 1] + n * a.ld_w + 16 * piece;
+  }
+  const int sz = HALVES == 2 ? lane >> 4 & 1 : 1;
+  const int sn = HALVES == 2 ? (lane >> 5) * 16 + (lane & 15) : lane;
+  const uint8_t* sp = a.s[sz] + (int64_t)min(n0 + sn, a.n - 1) * 4;
+  const uint8_t* xp[XR / 4];
+  int cell[XR / 4];
+#pragma unroll
+  for (int i = 0; i < XR / 4; ++i) {
+    const int row = 4 * i + (lane >> 4);
+    cell[i] = (lane & 15) ^ (row & 15);
+    xp[i] = static_cast<const uint8_t*>(a.x) + min(m0 + row, a.m - 1) * a.ld_x * 2 + 16 * cell[i];
+  }
+  x8 held[DIRECT ? 1 : XR / 4];
+  auto load_x = [&](int b) {
+    if constexpr (!DIRECT)
+#pragma unroll
+      for (int i = 0; i < XR / 4; ++i)
+        held[i] = load_x8(reinterpret_cast<const T*>(xp[i]) + (int64_t)b * kF4Block, 0,
+                          a.k - b * kF4Block - 8 * cell[i]);
+  };
+  auto load = [&](int b, int turn) {
+    const uint32_t to = to0 + turn * STAGE;
+    const bool whole = (b + 1) * kF4Block <= a.k;
+#pragma unroll
+    for (int z = 0; z < NT; ++z) {
+      const uint8_t* p = wp[z] + (int64_t)b * 64;
+      load_lds16(whole || b * kF4Block + 32 * piece < a.k ? (const void*)p : g_zero, to + 1024 * z);
+    }
+    if (lane < 16 * NT) load_lds4(sp + (int64_t)b * a.n * 4, to + 1024 * NT);
+    if constexpr (DIRECT)
+#pragma unroll
+      for (int i = 0; i < XR / 4; ++i) {
+        const uint8_t* p = xp[i] + (int64_t)b * (2 * kF4Block);
+        load_lds16(whole || b * kF4Block + 8 * cell[i] < a.k ? (const void*)p : g_zero,
+                   to + 1024 * NT + 256 + 1024 * i);
+      }
+  };
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int z = 0; z < NT; ++z)
+#pragma unroll
+    for (int x = 0; x < MT; ++x) acc[z][x] = f32x4{0, 0, 0, 0};
+  const int mine = wave < a.kb ? (a.kb - wave + waves - 1) / waves : 0;     // blocks
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < mine) load(wave + i * waves, i);
+  if (mine) load_x(wave);
+  int turn = 0;
+  for (int t = 0; t < mine; ++t, turn = turn + 1 == AHEAD ? 0 : turn + 1) {
+    const int b = wave + t * waves;
+    uint8_t* at = own + turn * STAGE;
+    uint8_t* xs = at + 1024 * NT + 256;
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int i = 0; i < XR / 4; ++i)
+        *reinterpret_cast<x8*>(xs + 1024 * i + 16 * lane) = held[i];
+      if (t + 1 < mine) load_x(b + waves);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+      wait_loads<LOADS, AHEAD - 1>(mine - 1 - t);
+    }
+    // groups past k, whatever their bytes
+    const uint32_t keep =
+        (b + 1) * kF4Block <= a.k ? ~0u : ~0u >> (8 * (3 - (a.k - 1) % kF4Block / 32));
+    x8 xv[MT][4];
+#pragma unroll
+    for (int x = 0; x < MT; ++x) {
+      const int row = 16 * x + (XR < 16 ? r & (XR - 1) : r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        xv[x][e] = *reinterpret_cast<const x8*>(xs + 256 * row + 16 * ((4 * g + e) ^ (row & 15)));
+    }
+#pragma unroll
+    for (int z = 0; z < NT; ++z) {
+      const u32x4 words =
+          *reinterpret_cast<const u32x4*>(at + 1024 * z + 64 * r + 16 * (g ^ (r >> 2)));
+      const uint32_t four = *reinterpret_cast<const uint32_t*>(at + 1024 * NT + 4 * (16 * z + r));
+      const float scale = f4_scale((four & keep) >> (8 * g) & 255u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const x8 wv = operand<T>(words[e], scale);
+#pragma unroll
+        for (int x = 0; x < MT; ++x) acc[z][x] = Half<T>::mma16(wv, xv[x][e], acc[z][x]);
+      }
+    }
+    // read, before it is loaded over
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (t + AHEAD < mine) load(b + AHEAD * waves, turn);
+  }
+  __syncthreads();                                 // the sums lie where the stages did
+  f32x4* sums = reinterpret_cast<f32x4*>(few_lds);
+#pragma unroll
+  for (int z = 0; z < NT; ++z)
+#pragma unroll
+    for (int x = 0; x < MT; ++x) sums[((wave * NT + z) * MT + x) * 64 + lane] = acc[z][x];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * MT * NT / HALVES; i += blockDim.x) {
+    const int l = i & 63, x = (i >> 6) % MT, q = (i >> 6) / MT;
+    const int n = n0 + 16 * q + 4 * (l >> 4), m = m0 + 16 * x + (l & 15);
+    if (m >= a.m || n >= a.n) continue;
+    f32x4 v[HALVES];
+#pragma unroll
+    for (int z = 0; z < HALVES; ++z) {
+      const f32x4* p = sums + ((HALVES * q + z) * MT + x) * 64 + l;
+      v[z] = *p;
+      for (int w = 1; w < waves; ++w) v[z] += p[w * NT * MT * 64];
+    }
+    if constexpr (HALVES == 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[0][e] = activate(v[0][e], a.activation) * v[1][e];
+    store4(a.y, a.y_type, m * a.ld_y + n, v[0], a.n - n);
+  }
 }
 
 // Many activation rows: a workgroup takes 32 * MT of them, in LDS, and its WN
@@ -396,7 +495,7 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs 
       } else {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
-          load_lds16(b * kF4Block + 8 * cell[i] < a.k ? (const void*)(base + xoff[i]) : &g_zero,
+          load_lds16(b * kF4Block + 8 * cell[i] < a.k ? (const void*)(base + xoff[i]) : g_zero,
                      to + 1024 * i);
       }
     } else {
@@ -535,27 +634,56 @@ enum Way { kRows, kTiles };
 
 struct Plan {
   Way way;
+  int32_t xr, nt;    // few rows: activation rows, and tiles of 16 weight rows
+  int32_t waves;     // few rows: waves that share k
   int32_t halves;    // tiles: groups of waves that share k
   int64_t groups;    // workgroups
 };
 
+// LDS of a wave: its stages, and then its sums.
+int few_lds_bytes(int xr, int nt) {
+  return std::max(few_ahead(xr) * few_stage(xr, nt), (xr + 15) / 16 * nt * 1024);
+}
+
 Plan plan_of(const ifq_f4_matmul_desc& d) {
-  const int each = d.activation ? 128 : 256;       // columns of y for a tile
-  Plan p = {d.m > 64 ? kTiles : kRows, 1, 0};
+  const int halves = d.activation ? 2 : 1;
+  const int64_t kb = ceil_of(d.k, kF4Block);
+  Plan p = {d.m > 64 ? kTiles : kRows, 4, 1, 4, 1, 0};
   if (p.way == kRows) {
-    p.groups = ceil_of(d.m, 32) * ceil_of(d.n, 16);
+    p.xr = d.m <= 4 ? 4 : d.m <= 8 ? 8 : (int32_t)std::min<int64_t>(64, 16 * ceil_of(d.m, 16));
+    p.nt = p.xr <= 16 && halves == 1 ? 1 : 2;
+    p.groups = ceil_of(d.m, p.xr) * ceil_of(d.n, 16 * p.nt / halves);
+    if (p.groups <= 512 && kb >= 8) p.waves = 8;
+    p.waves = std::min(p.waves, kLdsBytes / few_lds_bytes(p.xr, p.nt));
   } else {
-    p.groups = ceil_of(d.m, 128) * ceil_of(d.n, each);
+    p.groups = ceil_of(d.m, 128) * ceil_of(d.n, 256 / halves);
     if (p.groups <= 256 && d.k >= 1024) p.halves = 2;
   }
   return p;
 }
 
-template <typename T, int HALVES>
+template <typename T, int XR, int NT, int HALVES, bool DIRECT>
+void few_of(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
+  a.groups_n = (int32_t)ceil_of(a.n, 16 * NT / HALVES);
+  hipLaunchKernelGGL((f4_matmul_few<T, XR, NT, HALVES, DIRECT>), dim3((uint32_t)p.groups),
+                     dim3(64 * p.waves), few_lds_bytes(XR, NT) * p.waves, stream, a);
+}
+
+template <typename T, int HALVES, bool DIRECT>
 void few(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
-  a.groups_n = (a.n + 15) / 16;
-  const dim3 grid((uint32_t)p.groups), block(256);
-  hipLaunchKernelGGL((f4_matmul_few<T, 2, 4, HALVES>), grid, block, 0, stream, a);
+  if (HALVES == 1 && p.nt == 1) {
+    if (p.xr == 4) return few_of<T, 4, 1, 1, DIRECT>(a, p, stream);
+    if (p.xr == 8) return few_of<T, 8, 1, 1, DIRECT>(a, p, stream);
+    return few_of<T, 16, 1, 1, DIRECT>(a, p, stream);
+  }
+  switch (p.xr) {
+    case 4: return few_of<T, 4, 2, HALVES, DIRECT>(a, p, stream);
+    case 8: return few_of<T, 8, 2, HALVES, DIRECT>(a, p, stream);
+    case 16: return few_of<T, 16, 2, HALVES, DIRECT>(a, p, stream);
+    case 32: return few_of<T, 32, 2, HALVES, DIRECT>(a, p, stream);
+    case 48: return few_of<T, 48, 2, HALVES, DIRECT>(a, p, stream);
+    default: return few_of<T, 64, 2, HALVES, DIRECT>(a, p, stream);
+  }
 }
 
 template <typename T, int HALVES, bool DIRECT>
@@ -572,10 +700,11 @@ void tiled(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
 
 template <typename T, int HALVES>
 void matmul(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
-  if (p.way == kRows) return few<T, HALVES>(a, p, stream);
   // whole cells of 16 bytes, and 32-bit offsets within the rows of a tile
   const bool direct = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.ld_x % 8 == 0 &&
                       a.k % 8 == 0 && a.ld_x <= (1 << 22);
+  if (p.way == kRows)
+    return direct ? few<T, HALVES, true>(a, p, stream) : few<T, HALVES, false>(a, p, stream);
   if (direct) tiled<T, HALVES, true>(a, p, stream);
   else tiled<T, HALVES, false>(a, p, stream);
 }
@@ -643,7 +772,18 @@ int64_t f4_matmul_groups(const ifq_f4_matmul_desc& d) {
 const char* f4_matmul_kernel_name(const ifq_f4_matmul_desc& d) {
   if (d.m == 0 || d.n == 0) return "";
   const Plan p = plan_of(d);
-  if (p.way == kRows) return d.activation ? "f4_matmul_few<2, 4, 2>" : "f4_matmul_few<2, 4, 1>";
+  if (p.way == kRows) {
+    const int i = p.xr <= 16 ? p.xr / 8 : p.xr / 16 + 1;       // 4, 8, 16, 32, 48, 64
+    static const char* const narrow[] = {"f4_matmul_few<4, 1, 1>", "f4_matmul_few<8, 1, 1>",
+                                         "f4_matmul_few<16, 1, 1>"};
+    static const char* const one[] = {"f4_matmul_few<4, 2, 1>",  "f4_matmul_few<8, 2, 1>",
+                                      "f4_matmul_few<16, 2, 1>", "f4_matmul_few<32, 2, 1>",
+                                      "f4_matmul_few<48, 2, 1>", "f4_matmul_few<64, 2, 1>"};
+    static const char* const two[] = {"f4_matmul_few<4, 2, 2>",  "f4_matmul_few<8, 2, 2>",
+                                      "f4_matmul_few<16, 2, 2>", "f4_matmul_few<32, 2, 2>",
+                                      "f4_matmul_few<48, 2, 2>", "f4_matmul_few<64, 2, 2>"};
+    return p.nt == 1 ? narrow[i] : (d.activation ? two : one)[i];
+  }
   if (p.halves == 2)
     return d.activation ? "f4_matmul_tiled<4, 2, 4, 2, 2>" : "f4_matmul_tiled<4, 2, 4, 2, 1>";
   return d.activation ? "f4_matmul_tiled<4, 2, 4, 1, 2>" : "f4_matmul_tiled<4, 2, 4, 1, 1>";
