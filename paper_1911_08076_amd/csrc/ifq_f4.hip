@@ -240,9 +240,8 @@ __device__ __forceinline__ typename Half<T>::x8 load_x8(const T* row, int c, int
   return v;
 }
 
-// Stages of LDS of a wave of few rows: weights, scales, x; and how many there are.
-constexpr int few_stage(int xr, int nt) { return 1024 * nt + 256 + 256 * xr; }
-constexpr int few_ahead(int xr) { return xr <= 8 ? 4 : xr <= 16 ? 3 : 2; }
+// A stage of LDS of a group of `wn` waves of few rows: x, and each wave's weights and scales.
+constexpr int few_stage(int xr, int nt, int wn) { return 256 * xr + wn * (1024 * nt + 256); }
 constexpr int kLdsBytes = 160 * 1024;
 
 // Zeros: what loads past the end of a row read.
@@ -287,35 +286,46 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
   return reinterpret_cast<const uint8_t*>((uintptr_t)((uint64_t)hi << 32 | lo));
 }
 
-// Few activation rows. A workgroup takes 16 * NT weight rows (of both halves
-// together, where HALVES is 2) and XR activation rows, its waves every so many-th
-// block of 128 columns; the waves' sums are added in LDS in their order.
+__device__ __forceinline__ int turned(int q) { return (q & 1) << 1 ^ (q >> 1 & 1) * 3; }
+
+// Few activation rows. A workgroup takes 16 * NT * WN weight rows (of both halves
+// together, where HALVES is 2) and XR activation rows. Its waves are groups of WN, which
+// share their rows of x; a group takes every so many-th block of 128 columns, and the
+// groups' sums are added in LDS in their order.
 //
-// A wave brings its blocks through LDS of its own, AHEAD of them on their way at a time:
-// there consecutive lanes read consecutive 16 bytes of a row, 64 of weights and 256
-// of x, where the operands' own order (16 lanes in 16 rows) takes a cycle for each lane
-// (7 x 128000 x 4096 102 us, 32 x 4096 x 14336 34). Rows of weights lie 64 bytes
-// apart with group c at place c ^ (r / 4 & 3), rows of x 256 with cell c at c ^ (r & 15):
-// the 16 rows of which a read takes 16 bytes each at a time spread over all 64 banks.
+// All operands come through LDS, STAGES blocks of a group there at a time: then
+// consecutive lanes read consecutive 16 bytes of a row, 64 of weights and 256 of x, where
+// the operands' own order (16 lanes in 16 rows) takes a cycle for each lane (7 x 128000 x
+// 4096 102 us, 32 x 4096 x 14336 34). Rows of weights lie 64 bytes apart with group c at
+// place c ^ turned(r / 4), rows of x 256 with cell c at c ^ (r & 3) ^ 4 turned(r / 4): a
+// read takes 16 lanes at a time (0-3, 12-15, 20-27 and so on), here rows 0-3 and 12-15
+// of one group and 4-11 of the next, and these then spread over all 64 banks.
 //
 // DIRECT: x goes from memory into LDS; it needs 16-byte aligned rows of whole cells.
 // Otherwise it goes through registers, a block ahead.
-template <typename T, int XR, int NT, int HALVES, bool DIRECT>
-__global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
+template <typename T, int XR, int NT, int WN, int STAGES, int HALVES, bool DIRECT>
+__global__ __launch_bounds__(XR <= 16 ? 1024 : 512) void f4_matmul_few(F4MatmulArgs a) {
   constexpr int MT = (XR + 15) / 16, COLUMNS = 16 * NT / HALVES;
-  constexpr int AHEAD = few_ahead(XR), STAGE = few_stage(XR, NT);
-  constexpr int LOADS = NT + 1 + (DIRECT ? XR / 4 : 0);
-  extern __shared__ __align__(16) uint8_t few_lds[];        // [wave][AHEAD][STAGE], then sums
+  constexpr int WB = 1024 * NT + 256, STAGE = few_stage(XR, NT, WN);
+  constexpr int XL = XR / 4 / WN;                  // loads of 4 rows of x, for a wave
+  static_assert(XL * 4 * WN == XR, "");
+  constexpr int LOADS = NT + 1 + (DIRECT ? XL : 0);
+  // a group of one wave loads a stage over as soon as it has read it, others after the next
+  // barrier
+  constexpr int AHEAD = WN == 1 ? STAGES : STAGES - 1;
+  extern __shared__ __align__(16) uint8_t few_lds[];        // [group][STAGES][STAGE], then sums
   typedef typename Half<T>::x8 x8;
-  const int waves = blockDim.x >> 6;
+  const int groups = (blockDim.x >> 6) / WN;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = wave / WN, wn = wave % WN;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x % a.groups_n * COLUMNS, m0 = blockIdx.x / a.groups_n * XR;
-  uint8_t* const own = few_lds + wave * (AHEAD * STAGE);
+  const int n0 = (blockIdx.x % a.groups_n * WN + wn) * COLUMNS;
+  const int m0 = blockIdx.x / a.groups_n * XR;
+  uint8_t* const own = few_lds + group * (STAGES * STAGE);
   const uint32_t to0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)own;
   // what this lane loads: group `piece` of row lane / 4, scales of row lane, and
-  // cell `cell` of rows 4 i + lane / 16
-  const int piece = (lane & 3) ^ (lane >> 4 & 3);
+  // cell `cell` of this wave's rows 4 i + lane / 16
+  const int piece = (lane & 3) ^ turned(lane >> 4);
   const uint8_t* wp[NT];
 #pragma unroll
   for (int z = 0; z < NT; ++z) {
@@ -325,37 +335,38 @@ __global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
   const int sz = HALVES == 2 ? lane >> 4 & 1 : 1;
   const int sn = HALVES == 2 ? (lane >> 5) * 16 + (lane & 15) : lane;
   const uint8_t* sp = a.s[sz] + (int64_t)min(n0 + sn, a.n - 1) * 4;
-  const uint8_t* xp[XR / 4];
-  int cell[XR / 4];
+  const uint8_t* xp[XL];
+  int cell[XL];
 #pragma unroll
-  for (int i = 0; i < XR / 4; ++i) {
-    const int row = 4 * i + (lane >> 4);
-    cell[i] = (lane & 15) ^ (row & 15);
+  for (int i = 0; i < XL; ++i) {
+    const int row = 4 * (XL * wn + i) + (lane >> 4);
+    cell[i] = (lane & 15) ^ (row & 3) ^ 4 * turned(row >> 2);
     xp[i] = static_cast<const uint8_t*>(a.x) + min(m0 + row, a.m - 1) * a.ld_x * 2 + 16 * cell[i];
   }
-  x8 held[DIRECT ? 1 : XR / 4];
+  x8 held[DIRECT ? 1 : XL];
   auto load_x = [&](int b) {
     if constexpr (!DIRECT)
 #pragma unroll
-      for (int i = 0; i < XR / 4; ++i)
+      for (int i = 0; i < XL; ++i)
         held[i] = load_x8(reinterpret_cast<const T*>(xp[i]) + (int64_t)b * kF4Block, 0,
                           a.k - b * kF4Block - 8 * cell[i]);
   };
   auto load = [&](int b, int turn) {
-    const uint32_t to = to0 + turn * STAGE;
+    const uint32_t to = to0 + turn * STAGE, tw = to + 256 * XR + WB * wn;
     const bool whole = (b + 1) * kF4Block <= a.k;
 #pragma unroll
     for (int z = 0; z < NT; ++z) {
       const uint8_t* p = wp[z] + (int64_t)b * 64;
-      load_lds16(whole || b * kF4Block + 32 * piece < a.k ? (const void*)p : g_zero, to + 1024 * z);
+      load_lds16(whole || b * kF4Block + 32 * piece < a.k ? (const void*)p : g_zero,
+                 tw + 1024 * z);
     }
-    if (lane < 16 * NT) load_lds4(sp + (int64_t)b * a.n * 4, to + 1024 * NT);
+    if (lane < 16 * NT) load_lds4(sp + (int64_t)b * a.n * 4, tw + 1024 * NT);
     if constexpr (DIRECT)
 #pragma unroll
-      for (int i = 0; i < XR / 4; ++i) {
+      for (int i = 0; i < XL; ++i) {
         const uint8_t* p = xp[i] + (int64_t)b * (2 * kF4Block);
         load_lds16(whole || b * kF4Block + 8 * cell[i] < a.k ? (const void*)p : g_zero,
-                   to + 1024 * NT + 256 + 1024 * i);
+                   to + 1024 * (XL * wn + i));
       }
   };
   f32x4 acc[NT][MT];
@@ -363,24 +374,35 @@ __global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
   for (int z = 0; z < NT; ++z)
 #pragma unroll
     for (int x = 0; x < MT; ++x) acc[z][x] = f32x4{0, 0, 0, 0};
-  const int mine = wave < a.kb ? (a.kb - wave + waves - 1) / waves : 0;     // blocks
+  const int mine = group < a.kb ? (a.kb - group + groups - 1) / groups : 0;     // blocks
+  const int turns = WN == 1 ? mine : (a.kb + groups - 1) / groups;
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
-    if (i < mine) load(wave + i * waves, i);
-  if (mine) load_x(wave);
+    if (i < mine) load(group + i * groups, i);
+  if (mine) load_x(group);
   int turn = 0;
-  for (int t = 0; t < mine; ++t, turn = turn + 1 == AHEAD ? 0 : turn + 1) {
-    const int b = wave + t * waves;
-    uint8_t* at = own + turn * STAGE;
-    uint8_t* xs = at + 1024 * NT + 256;
+  for (int t = 0; t < turns; ++t, turn = turn + 1 == STAGES ? 0 : turn + 1) {
+    const int b = group + t * groups;
+    uint8_t* const xs = own + turn * STAGE;
+    uint8_t* const ws = xs + 256 * XR + WB * wn;
     if constexpr (!DIRECT) {
+      if (t < mine) {
 #pragma unroll
-      for (int i = 0; i < XR / 4; ++i)
-        *reinterpret_cast<x8*>(xs + 1024 * i + 16 * lane) = held[i];
-      if (t + 1 < mine) load_x(b + waves);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        for (int i = 0; i < XL; ++i)
+          *reinterpret_cast<x8*>(xs + 1024 * (XL * wn + i) + 16 * lane) = held[i];
+        if (t + 1 < mine) load_x(b + groups);
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     } else {
       wait_loads<LOADS, AHEAD - 1>(mine - 1 - t);
+    }
+    if constexpr (WN > 1) {
+      // the stage is there for all its waves, and the last one is read
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (t + AHEAD < mine) load(b + AHEAD * groups, turn == 0 ? STAGES - 1 : turn - 1);
+      if (t >= mine) break;                        // the last barrier of a group with a block less
     }
     // groups past k, whatever their bytes
     const uint32_t keep =
@@ -389,15 +411,16 @@ __global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
 #pragma unroll
     for (int x = 0; x < MT; ++x) {
       const int row = 16 * x + (XR < 16 ? r & (XR - 1) : r);
+      const int swap = (row & 3) ^ 4 * turned(row >> 2);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        xv[x][e] = *reinterpret_cast<const x8*>(xs + 256 * row + 16 * ((4 * g + e) ^ (row & 15)));
+        xv[x][e] = *reinterpret_cast<const x8*>(xs + 256 * row + 16 * ((4 * g + e) ^ swap));
     }
 #pragma unroll
     for (int z = 0; z < NT; ++z) {
       const u32x4 words =
-          *reinterpret_cast<const u32x4*>(at + 1024 * z + 64 * r + 16 * (g ^ (r >> 2)));
-      const uint32_t four = *reinterpret_cast<const uint32_t*>(at + 1024 * NT + 4 * (16 * z + r));
+          *reinterpret_cast<const u32x4*>(ws + 1024 * z + 64 * r + 16 * (g ^ turned(r >> 2)));
+      const uint32_t four = *reinterpret_cast<const uint32_t*>(ws + 1024 * NT + 4 * (16 * z + r));
       const float scale = f4_scale((four & keep) >> (8 * g) & 255u);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -406,9 +429,11 @@ __global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
         for (int x = 0; x < MT; ++x) acc[z][x] = Half<T>::mma16(wv, xv[x][e], acc[z][x]);
       }
     }
-    // read, before it is loaded over
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (t + AHEAD < mine) load(b + AHEAD * waves, turn);
+    if constexpr (WN == 1) {
+      // read, before it is loaded over
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (t + AHEAD < mine) load(b + AHEAD * groups, turn);
+    }
   }
   __syncthreads();                                 // the sums lie where the stages did
   f32x4* sums = reinterpret_cast<f32x4*>(few_lds);
@@ -417,16 +442,16 @@ __global__ __launch_bounds__(512) void f4_matmul_few(F4MatmulArgs a) {
 #pragma unroll
     for (int x = 0; x < MT; ++x) sums[((wave * NT + z) * MT + x) * 64 + lane] = acc[z][x];
   __syncthreads();
-  for (int i = threadIdx.x; i < 64 * MT * NT / HALVES; i += blockDim.x) {
-    const int l = i & 63, x = (i >> 6) % MT, q = (i >> 6) / MT;
-    const int n = n0 + 16 * q + 4 * (l >> 4), m = m0 + 16 * x + (l & 15);
+  for (int i = threadIdx.x; i < 64 * MT * NT / HALVES * WN; i += blockDim.x) {
+    const int l = i & 63, x = (i >> 6) % MT, q = (i >> 6) / MT;       // q: 16 columns of y
+    const int n = n0 - wn * COLUMNS + 16 * q + 4 * (l >> 4), m = m0 + 16 * x + (l & 15);
     if (m >= a.m || n >= a.n) continue;
     f32x4 v[HALVES];
 #pragma unroll
     for (int z = 0; z < HALVES; ++z) {
       const f32x4* p = sums + ((HALVES * q + z) * MT + x) * 64 + l;
       v[z] = *p;
-      for (int w = 1; w < waves; ++w) v[z] += p[w * NT * MT * 64];
+      for (int w = 1; w < groups; ++w) v[z] += p[w * WN * NT * MT * 64];
     }
     if constexpr (HALVES == 2)
 #pragma unroll
@@ -546,10 +571,11 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs 
     store_x(0);
   }
   int turn = 0;
-  for (int b = half; b < a.kb + half; b += WK, turn ^= 1) {
+  for (int b0 = 0; b0 < a.kb; b0 += WK, turn ^= 1) {
+    const int b = b0 + half;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (WK > 1 && b >= a.kb) break;              // the last wait of a half with a block less
+    if (WK > 1 && b >= a.kb) break;              // the last wait of a group with a block less
     // taken before the next loads: the compiler's wait for these costs nothing here, and
     // later would count the loads into LDS
     u32x4 codes[NT][2];
@@ -587,7 +613,9 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs 
     if (more) store_x(turn ^ 1);
   }
   if constexpr (WK > 1) {
-    static_assert(WK == 2 && sizeof(lds) >= sizeof(float) * 64 * WN * MT * NT * 16, "");
+    // the other groups' sums are added to the first's in their order
+    constexpr int SIZE = MT * NT * 16 * 64 * WN;
+    static_assert(sizeof(lds) >= sizeof(float) * SIZE * (WK - 1), "");
     __syncthreads();
     float* sums = reinterpret_cast<float*>(&lds[0][0][0][0]) + threadIdx.x % (64 * WN);
     if (half) {
@@ -596,16 +624,20 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs 
 #pragma unroll
         for (int z = 0; z < NT; ++z)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sums[((x * NT + z) * 16 + e) * 64 * WN] = acc[x][z][e];
+          for (int e = 0; e < 16; ++e)
+            sums[(half - 1) * SIZE + ((x * NT + z) * 16 + e) * 64 * WN] = acc[x][z][e];
     }
     __syncthreads();
     if (half) return;
 #pragma unroll
-    for (int x = 0; x < MT; ++x)
+    for (int q = 0; q < WK - 1; ++q)
 #pragma unroll
-      for (int z = 0; z < NT; ++z)
+      for (int x = 0; x < MT; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[x][z][e] += sums[((x * NT + z) * 16 + e) * 64 * WN];
+        for (int z = 0; z < NT; ++z)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            acc[x][z][e] += sums[q * SIZE + ((x * NT + z) * 16 + e) * 64 * WN];
   }
 #pragma unroll
   for (int x = 0; x < MT; ++x) {
@@ -632,65 +664,119 @@ int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 enum Way { kRows, kTiles };
 
+// The kernels of few rows: rows of x, tiles of 16 weight rows of a wave, waves that share x,
+// stages, halves.
+#define IFQ_F4_FEW(F)                                                              \
+  F(4, 1, 1, 4, 1) F(4, 2, 1, 4, 1) F(8, 1, 1, 4, 1) F(8, 2, 1, 4, 1)               \
+  F(8, 2, 2, 4, 1) F(16, 1, 1, 3, 1) F(16, 2, 1, 3, 1) F(16, 2, 2, 4, 1)            \
+  F(16, 2, 4, 4, 1) F(32, 2, 1, 2, 1) F(32, 2, 2, 3, 1) F(32, 2, 4, 3, 1)           \
+  F(48, 2, 1, 2, 1) F(48, 2, 2, 3, 1) F(48, 2, 4, 3, 1) F(64, 2, 1, 2, 1)           \
+  F(64, 2, 2, 3, 1) F(64, 2, 4, 3, 1)                                               \
+  F(4, 2, 1, 4, 2) F(8, 2, 1, 4, 2) F(8, 2, 2, 4, 2) F(16, 2, 1, 3, 2)              \
+  F(16, 2, 2, 4, 2) F(16, 2, 4, 4, 2) F(32, 2, 1, 2, 2) F(32, 2, 2, 3, 2)           \
+  F(32, 2, 4, 3, 2) F(48, 2, 1, 2, 2) F(48, 2, 2, 3, 2) F(48, 2, 4, 3, 2)           \
+  F(64, 2, 1, 2, 2) F(64, 2, 2, 3, 2) F(64, 2, 4, 3, 2)
+
+struct Few {
+  int32_t xr, nt, wn, stages, halves;
+  const char* name;
+};
+
+constexpr Few kFew[] = {
+#define F(XR, NT, WN, ST, HV) \
+  {XR, NT, WN, ST, HV, "f4_matmul_few<" #XR ", " #NT ", " #WN ", " #ST ", " #HV ">"},
+    IFQ_F4_FEW(F)
+#undef F
+};
+
 struct Plan {
   Way way;
-  int32_t xr, nt;    // few rows: activation rows, and tiles of 16 weight rows
-  int32_t waves;     // few rows: waves that share k
-  int32_t halves;    // tiles: groups of waves that share k
+  int32_t few;       // few rows: index in kFew
+  int32_t shares;    // groups of waves that share k
   int64_t groups;    // workgroups
 };
 
-// LDS of a wave: its stages, and then its sums.
-int few_lds_bytes(int xr, int nt) {
-  return std::max(few_ahead(xr) * few_stage(xr, nt), (xr + 15) / 16 * nt * 1024);
+// LDS of a group of waves: its stages, and then its sums.
+int few_lds_bytes(const Few& f) {
+  return std::max(f.stages * few_stage(f.xr, f.nt, f.wn), (f.xr + 15) / 16 * f.nt * f.wn * 1024);
+}
+
+int64_t few_groups(const ifq_f4_matmul_desc& d, const Few& f) {
+  return ceil_of(d.m, f.xr) * ceil_of(d.n, 16 * f.nt * f.wn / f.halves);
+}
+
+// Time in us of a kernel of few rows with k shared by `shares` groups of waves: a round of
+// workgroups is its start and end and its turns, each as long as the loads on their way
+// take or as what a CU's workgroups load (KB) and read in LDS. Fitted to 3900 times of
+// 260 sizes (m up to 1300, n from 100 to 128000, k from 64 to 14336) with 11 % between
+// them on the mean; the choice by it takes 1.5 % longer than the best of the kernels,
+// 35 % at worst (6 x 12717 x 10888 gated 54.6 and 42.1).
+float few_time(const Few& f, int lds, int64_t groups, int64_t kb, int shares) {
+  const int64_t each = (groups + 255) / 256;       // on the busiest CU
+  const int64_t fit = std::max(1, std::min(kLdsBytes / (lds * shares), 16 / (shares * f.wn)));
+  const int64_t at_once = std::min(fit, each), rounds = (each + at_once - 1) / at_once;
+  const float load = (float)(shares * few_stage(f.xr, f.nt, f.wn)) / 1024;
+  const float read = (float)(shares * f.wn * (f.xr + 4 * f.nt)) / 4;
+  const float turn = std::max(1.43f / (float)(f.wn == 1 ? f.stages : f.stages - 1),
+                              (float)at_once * (0.009f * load + 0.0045f * read));
+  return 0.5f + (float)rounds * (2.4f + 0.023f * (float)(shares * f.wn * f.nt * ((f.xr + 15) / 16)) +
+                                 (float)((kb + shares - 1) / shares) * turn);
+}
+
+// And of tiles of 128 rows, alone on a CU or in pairs.
+float tiles_time(int64_t groups, int64_t kb, int shares) {
+  if (shares == 2) return 9.8f + 2.8f * (float)((kb + 1) / 2);
+  const int64_t rest = groups % 512;
+  return 7.2f + 0.4f * (float)((groups + 511) / 512) +
+         (float)kb * (3.2f * (float)(groups / 512) + (rest == 0 ? 0.0f : rest <= 256 ? 1.6f : 3.2f));
 }
 
 Plan plan_of(const ifq_f4_matmul_desc& d) {
   const int halves = d.activation ? 2 : 1;
   const int64_t kb = ceil_of(d.k, kF4Block);
-  Plan p = {d.m > 64 ? kTiles : kRows, 4, 1, 4, 1, 0};
-  if (p.way == kRows) {
-    p.xr = d.m <= 4 ? 4 : d.m <= 8 ? 8 : (int32_t)std::min<int64_t>(64, 16 * ceil_of(d.m, 16));
-    p.nt = p.xr <= 16 && halves == 1 ? 1 : 2;
-    p.groups = ceil_of(d.m, p.xr) * ceil_of(d.n, 16 * p.nt / halves);
-    if (p.groups <= 512 && kb >= 8) p.waves = 8;
-    p.waves = std::min(p.waves, kLdsBytes / few_lds_bytes(p.xr, p.nt));
-  } else {
-    p.groups = ceil_of(d.m, 128) * ceil_of(d.n, 256 / halves);
-    if (p.groups <= 256 && d.k >= 1024) p.halves = 2;
+  Plan p = {kTiles, 0, 1, ceil_of(d.m, 128) * ceil_of(d.n, 256 / halves)};
+  if (p.groups <= 256 && kb >= 2) p.shares = 2;
+  float best = d.m <= 32 ? 1e30f : tiles_time(p.groups, kb, p.shares);
+  // as many rows of x as there are, or 48 and 64 of more
+  const int xr = d.m <= 4 ? 4 : d.m <= 8 ? 8 : d.m <= 64 ? (int)ceil_of(d.m, 16) * 16 : 0;
+  for (int i = 0; i < (int)(sizeof(kFew) / sizeof(kFew[0])); ++i) {
+    const Few& f = kFew[i];
+    if (f.halves != halves || (xr ? f.xr != xr : f.xr < 48)) continue;
+    const int lds = few_lds_bytes(f);
+    const int64_t groups = few_groups(d, f);
+    for (int shares = 8 / f.wn; shares >= 1; shares /= 2) {
+      const int some = (int)std::min<int64_t>(std::min(shares, kLdsBytes / lds), kb);
+      const float t = few_time(f, lds, groups, kb, some);
+      if (t < best) best = t, p = {kRows, i, some, groups};
+    }
   }
   return p;
 }
 
-template <typename T, int XR, int NT, int HALVES, bool DIRECT>
+template <typename T, int XR, int NT, int WN, int STAGES, int HALVES, bool DIRECT>
 void few_of(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
-  a.groups_n = (int32_t)ceil_of(a.n, 16 * NT / HALVES);
-  hipLaunchKernelGGL((f4_matmul_few<T, XR, NT, HALVES, DIRECT>), dim3((uint32_t)p.groups),
-                     dim3(64 * p.waves), few_lds_bytes(XR, NT) * p.waves, stream, a);
+  a.groups_n = (int32_t)ceil_of(a.n, 16 * NT * WN / HALVES);
+  hipLaunchKernelGGL((f4_matmul_few<T, XR, NT, WN, STAGES, HALVES, DIRECT>),
+                     dim3((uint32_t)p.groups), dim3(64 * WN * p.shares),
+                     few_lds_bytes(kFew[p.few]) * p.shares, stream, a);
 }
 
 template <typename T, int HALVES, bool DIRECT>
 void few(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
-  if (HALVES == 1 && p.nt == 1) {
-    if (p.xr == 4) return few_of<T, 4, 1, 1, DIRECT>(a, p, stream);
-    if (p.xr == 8) return few_of<T, 8, 1, 1, DIRECT>(a, p, stream);
-    return few_of<T, 16, 1, 1, DIRECT>(a, p, stream);
-  }
-  switch (p.xr) {
-    case 4: return few_of<T, 4, 2, HALVES, DIRECT>(a, p, stream);
-    case 8: return few_of<T, 8, 2, HALVES, DIRECT>(a, p, stream);
-    case 16: return few_of<T, 16, 2, HALVES, DIRECT>(a, p, stream);
-    case 32: return few_of<T, 32, 2, HALVES, DIRECT>(a, p, stream);
-    case 48: return few_of<T, 48, 2, HALVES, DIRECT>(a, p, stream);
-    default: return few_of<T, 64, 2, HALVES, DIRECT>(a, p, stream);
-  }
+  int i = 0;
+#define F(XR, NT, WN, ST, HV)                                                    \
+  if constexpr (HV == HALVES)                                                    \
+    if (p.few == i) return few_of<T, XR, NT, WN, ST, HV, DIRECT>(a, p, stream);  \
+  ++i;
+  IFQ_F4_FEW(F)
+#undef F
 }
 
 template <typename T, int HALVES, bool DIRECT>
 void tiled(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
   a.groups_m = (a.m + 127) / 128;
   const dim3 grid((uint32_t)p.groups);
-  if (p.halves == 2)
+  if (p.shares == 2)
     hipLaunchKernelGGL((f4_matmul_tiled<T, 4, 2, 4, 2, HALVES, DIRECT>), grid, dim3(512), 0,
                        stream, a);
   else
@@ -766,25 +852,17 @@ hipError_t launch_f4_dequantize(const ifq_f4_weights_desc& d, const void* codes,
 size_t f4_matmul_workspace_bytes(const ifq_f4_matmul_desc&) { return 0; }
 
 int64_t f4_matmul_groups(const ifq_f4_matmul_desc& d) {
-  return d.m == 0 || d.n == 0 ? 0 : plan_of(d).groups;
+  if (d.m == 0 || d.n == 0) return 0;
+  const Plan p = plan_of(d);
+  const int waves = p.way == kRows ? p.shares * kFew[p.few].wn : 4 * p.shares;
+  return ceil_of(p.groups * waves, 4);
 }
 
 const char* f4_matmul_kernel_name(const ifq_f4_matmul_desc& d) {
   if (d.m == 0 || d.n == 0) return "";
   const Plan p = plan_of(d);
-  if (p.way == kRows) {
-    const int i = p.xr <= 16 ? p.xr / 8 : p.xr / 16 + 1;       // 4, 8, 16, 32, 48, 64
-    static const char* const narrow[] = {"f4_matmul_few<4, 1, 1>", "f4_matmul_few<8, 1, 1>",
-                                         "f4_matmul_few<16, 1, 1>"};
-    static const char* const one[] = {"f4_matmul_few<4, 2, 1>",  "f4_matmul_few<8, 2, 1>",
-                                      "f4_matmul_few<16, 2, 1>", "f4_matmul_few<32, 2, 1>",
-                                      "f4_matmul_few<48, 2, 1>", "f4_matmul_few<64, 2, 1>"};
-    static const char* const two[] = {"f4_matmul_few<4, 2, 2>",  "f4_matmul_few<8, 2, 2>",
-                                      "f4_matmul_few<16, 2, 2>", "f4_matmul_few<32, 2, 2>",
-                                      "f4_matmul_few<48, 2, 2>", "f4_matmul_few<64, 2, 2>"};
-    return p.nt == 1 ? narrow[i] : (d.activation ? two : one)[i];
-  }
-  if (p.halves == 2)
+  if (p.way == kRows) return kFew[p.few].name;
+  if (p.shares == 2)
     return d.activation ? "f4_matmul_tiled<4, 2, 4, 2, 2>" : "f4_matmul_tiled<4, 2, 4, 2, 1>";
   return d.activation ? "f4_matmul_tiled<4, 2, 4, 1, 2>" : "f4_matmul_tiled<4, 2, 4, 1, 1>";
 }

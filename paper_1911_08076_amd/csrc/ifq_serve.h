@@ -54,7 +54,7 @@ hipError_t launch_f4_dequantize(const ifq_f4_weights_desc& d, const void* codes,
 
 // The product, and with an activation the gated one (w_gate is unused without).
 size_t f4_matmul_workspace_bytes(const ifq_f4_matmul_desc& d);
-int64_t f4_matmul_groups(const ifq_f4_matmul_desc& d);
+int64_t f4_matmul_groups(const ifq_f4_matmul_desc& d);   // its threads, in workgroups of 256
 const char* f4_matmul_kernel_name(const ifq_f4_matmul_desc& d);
 hipError_t launch_f4_matmul(const ifq_f4_matmul_desc& d, const void* x, const void* w_gate,
                             const void* gate_scales, const void* w, const void* w_scales,
