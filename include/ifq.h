@@ -1007,7 +1007,7 @@ IFQ_API ifq_status ifq_f4_gated(const ifq_f4_matmul_desc* d, const void* x, cons
  *   ld_x         elements from row to row of the logits, >= n
  *   ld_top       elements from row to row of top_logprobs and top_tokens, >= top
  *   x_type       IFQ_TYPE_BF16, F16 or F32
- *   top          0..64, at most n
+ *   top          0..64, at most n; 0 above 2^20 values (UNSUPPORTED)
  *   scale        0 < scale <= 2^64: one over the temperature
  *   reserved     0
  */

@@ -18,7 +18,9 @@ namespace {
 //
 // The top tokens go by a key of 64 bits: the value, as an integer of the same
 // order, over the complement of the index, so that keys differ and equal values
-// go by the lower index. A wave keeps its best 64 keys in order, one a lane.
+// go by the lower index. Of 256 groups of values the k-th largest maximum is a bar that k
+// values at least reach and few others: those are collected, and each one's place
+// is the number of larger ones.
 
 struct LogprobArgs {
   const void* x;
@@ -30,6 +32,7 @@ struct LogprobArgs {
   uint32_t* count;
   float* part;
   int64_t ld_x, ld_top;
+  int64_t row0;                  // first row of this launch
   int32_t n, top, parts;
   int32_t chunks;                // of a row, each a wave's turn
   float scale, c;
@@ -37,48 +40,82 @@ struct LogprobArgs {
 
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kWaves = 4;
-constexpr int kPer = 32;         // values of a lane in a turn
-constexpr int kTurn = 64 * kPer;
 constexpr int kPartFloats = 4;   // M, S, E of a part ahead of its keys
+constexpr int kMostParts = 32;   // of a row with top tokens
+constexpr int kMore = 3;         // maxima that may reach the bar beyond the top ones; LDS for two workgroups
 
-__device__ __forceinline__ uint64_t key_of(float v, int index) {
-  const uint32_t b = f32_bits(v + 0.0f);                  // -0 equals 0
-  const uint32_t order = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-  return (uint64_t)order << 32 | (uint32_t)~index;
+// The value of lane ^ D.
+template <int D>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  if constexpr (D == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);
+  if constexpr (D == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);
+  if constexpr (D == 4)          // 7 - i in eight lanes, then 3 - i in four
+    return __builtin_amdgcn_update_dpp(
+        0, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
+  if constexpr (D == 8) return __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, true);
+  if constexpr (D == 16) {
+    const auto both = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? both[0] : both[1];
+  }
+  const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return threadIdx.x & 32 ? both[0] : both[1];
 }
 
-__device__ __forceinline__ float value_of(uint64_t key) {
-  const uint32_t o = (uint32_t)(key >> 32);
-  return bits_f32(o >> 31 ? o ^ 0x80000000u : ~o);
+template <int D>
+__device__ __forceinline__ float lane_xor(float v) {
+  return bits_f32(lane_xor<D>(f32_bits(v)));
+}
+
+// An integer of the same order; -0 equals 0.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t b = f32_bits(v + 0.0f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+
+__device__ __forceinline__ float value_of(uint32_t order) {
+  return bits_f32(order >> 31 ? order ^ 0x80000000u : ~order);
+}
+
+__device__ __forceinline__ uint64_t key_of(float v, int index) {
+  return (uint64_t)order_of(v) << 32 | (uint32_t)~index;
 }
 
 __device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
 
-__device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
-  return (uint64_t)hi << 32 | lo;
-}
-
-// The list with one more key in its place; what falls off the last lane is lost.
-__device__ __forceinline__ uint64_t insert(uint64_t list, uint64_t key, int lane) {
-  const int place = __popcll(__ballot(list > key));
-  const uint64_t up = __shfl_up(list, 1);
-  return lane < place ? list : lane == place ? key : up;
-}
-
 struct Sums {
   float m, s, e;
-  // adds sums that go by another maximum
-  __device__ __forceinline__ void add(const Sums& o, float c) {
-    const float top = fmaxf(m, o.m), r = top == -INFINITY ? 0.0f : top;
+  // the sums as they go by a maximum that is as large at least
+  __device__ __forceinline__ void to(float top, float c) {
+    const float r = top == -INFINITY ? 0.0f : top;
     // an empty part has no share (and its maximum none either)
-    const float d0 = s == 0.0f ? 0.0f : c * (m - r), d1 = o.s == 0.0f ? 0.0f : c * (o.m - r);
-    const float f0 = __builtin_amdgcn_exp2f(d0), f1 = __builtin_amdgcn_exp2f(d1);
-    // a share of 0 adds nothing, also where d is -infinity
-    e = (f0 == 0.0f ? 0.0f : f0 * (e + d0 * s)) + (f1 == 0.0f ? 0.0f : f1 * (o.e + d1 * o.s));
-    s = f0 * s + f1 * o.s;
+    const float d = s == 0.0f ? 0.0f : c * (m - r), f = __builtin_amdgcn_exp2f(d);
+    e = f == 0.0f ? 0.0f : f * (e + d * s);    // a share of 0 adds nothing, also where d is -infinity
+    s *= f;
     m = top;
+  }
+  __device__ __forceinline__ void add(Sums o, float c) {
+    const float top = fmaxf(m, o.m);
+    to(top, c);
+    o.to(top, c);
+    s += o.s;
+    e += o.e;
+  }
+  // over the lanes
+  __device__ __forceinline__ void all(float c) {
+    float top = m;
+    top = fmaxf(top, lane_xor<1>(top));
+    top = fmaxf(top, lane_xor<2>(top));
+    top = fmaxf(top, lane_xor<4>(top));
+    top = fmaxf(top, lane_xor<8>(top));
+    top = fmaxf(top, lane_xor<16>(top));
+    top = fmaxf(top, lane_xor<32>(top));
+    to(top, c);
+    s += lane_xor<1>(s), e += lane_xor<1>(e);
+    s += lane_xor<2>(s), e += lane_xor<2>(e);
+    s += lane_xor<4>(s), e += lane_xor<4>(e);
+    s += lane_xor<8>(s), e += lane_xor<8>(e);
+    s += lane_xor<16>(s), e += lane_xor<16>(e);
+    s += lane_xor<32>(s), e += lane_xor<32>(e);
   }
 };
 
@@ -89,231 +126,391 @@ __device__ __forceinline__ int index_in_turn(int i, int lane) {
   return i / kRun<T> * (64 * kRun<T>) + lane * kRun<T> + i % kRun<T>;
 }
 
-// Values of a turn that starts at `base`; -infinity from n on. Rows may begin at any element.
-template <typename T>
+// Values of a turn that starts at `base`; -infinity from n on. Rows may begin at any
+// element. The loads of a row's last turn do not wait for one another either: runs past the
+// last whole one load that one again, and what is left of a run comes after.
+template <typename T, int PER>
 __device__ __forceinline__ void load_turn(const T* row, int base, int n, int lane, float* v) {
   constexpr int W = kRun<T>;
+  T t[PER];
+  if (base + 64 * PER <= n) {
 #pragma unroll
-  for (int i = 0; i < kPer; i += W) {
-    const int at = base + index_in_turn<T>(i, lane);
-    if (at + W <= n) {
-      T t[W];
-      __builtin_memcpy(t, row + at, sizeof(t));
+    for (int i = 0; i < PER; i += W)
+      __builtin_memcpy(t + i, row + base + index_in_turn<T>(i, lane), W * sizeof(T));
 #pragma unroll
-      for (int j = 0; j < W; ++j) v[i + j] = (float)t[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[i + j] = at + j < n ? (float)row[at + j] : -INFINITY;
-    }
+    for (int i = 0; i < PER; ++i) v[i] = (float)t[i];
+    return;
   }
+  const int rest = n % W, whole = n - rest;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = -INFINITY;
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < PER; i += W)
+      __builtin_memcpy(t + i, row + min(base + index_in_turn<T>(i, lane), whole - W), W * sizeof(T));
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (base + index_in_turn<T>(i - i % W, lane) < whole) v[i] = (float)t[i];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; i += W)
+    if (rest && base + index_in_turn<T>(i, lane) == whole) {
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        if (j < rest) v[i + j] = (float)row[whole + j];
+    }
 }
 
-// Takes a turn's values into the wave's list.
+// A turn's sums of a lane.
+template <int PER>
+__device__ __forceinline__ Sums sums_of(const float* v, float c) {
+  float m = v[0];
+#pragma unroll
+  for (int i = 1; i < PER; ++i) m = fmaxf(m, v[i]);
+  Sums u = {m, 0.0f, 0.0f};
+  const float r = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const float z = c * (v[i] - r), e = __builtin_amdgcn_exp2f(z);
+    u.s += e;
+    u.e = __builtin_fmaf(fmaxf(z, -1e4f), e, u.e);     // 0 where e is, z -infinity or not
+  }
+  return u;
+}
+
+// What a row's sums stand for. A row of -infinity alone has no probability anywhere (S is
+// 0); with a NaN or an infinity in it (S is NaN) it has no distribution.
+struct Row {
+  bool none;
+  float from, log;
+  __device__ __forceinline__ explicit Row(const Sums& t) {
+    const bool empty = t.s == 0.0f;
+    none = t.s != t.s;
+    from = empty ? 0.0f : t.m;
+    log = empty ? 0.0f : logf(t.s);
+  }
+  __device__ __forceinline__ float logprob(float v, float scale) const {
+    return scale * (v - from) - log;
+  }
+};
+
+// One lane's work.
 template <typename T>
-__device__ __forceinline__ uint64_t take_turn(uint64_t list, const float* v, int base, bool first,
-                                              int top, int lane) {
-  if (first) {
-    // the lanes' largest, in order: a list that few of the others get into
-    float best = v[0];
-    int at = 0;
-#pragma unroll
-    for (int i = 1; i < kPer; ++i)
-      if (v[i] > best) best = v[i], at = i;
-    const uint64_t own = key_of(best, base + index_in_turn<T>(at, lane));
-    int place = 0;
-    for (int j = 0; j < 64; ++j) place += lane_key(own, j) > own;
-    const int lo = __builtin_amdgcn_ds_permute(4 * place, (int)(uint32_t)own);
-    const int hi = __builtin_amdgcn_ds_permute(4 * place, (int)(uint32_t)(own >> 32));
-    list = (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
-    uint64_t bar = lane_key(list, top - 1);
-    const float bar_v = value_of(bar);
-    const int bar_i = index_of(bar) - base;
-    uint32_t mask = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      mask |= (v[i] > bar_v || (v[i] == bar_v && index_in_turn<T>(i, lane) < bar_i)) ? 1u << i : 0;
-    if (key_of(best, base + index_in_turn<T>(at, lane)) >= bar) mask &= ~(1u << at);  // there already
-    while (__ballot(mask != 0)) {
-      const int i = mask ? __ffs(mask) - 1 : 0;
-      float x = v[0];
-#pragma unroll
-      for (int j = 1; j < kPer; ++j) x = i == j ? v[j] : x;
-      const uint64_t key = mask ? key_of(x, base + index_in_turn<T>(i, lane)) : 0;
-      uint64_t left = __ballot(mask != 0);
-      while (left) {
-        const int from = __ffsll((unsigned long long)left) - 1;
-        left &= left - 1;
-        const uint64_t one = lane_key(key, from);
-        if (one > bar) {
-          list = insert(list, one, lane);
-          bar = lane_key(list, top - 1);
-        }
-      }
-      mask &= mask - 1;
-    }
-    return list;
+__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, const T* x, const Sums& t) {
+  const Row f(t);
+  if (a.entropy) a.entropy[row] = t.s == 0.0f ? 0.0f : f.log - kLn2 * (t.e / t.s);
+  if (a.logprob) {
+    const int token = a.tokens[row];
+    float p = 0.0f;
+    if (token >= a.n) p = bits_f32(0x7FC00000u);
+    else if (token >= 0) p = f.logprob((float)x[token], a.scale);
+    a.logprob[row] = p;
   }
-  // later turns hold higher indices: equal values stay out
-  uint64_t bar = lane_key(list, top - 1);
-  const float bar_v = value_of(bar);
-  uint32_t mask = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) mask |= v[i] > bar_v ? 1u << i : 0;
-  while (__ballot(mask != 0)) {
-    const int i = mask ? __ffs(mask) - 1 : 0;
-    float x = v[0];
-#pragma unroll
-    for (int j = 1; j < kPer; ++j) x = i == j ? v[j] : x;
-    const uint64_t key = mask ? key_of(x, base + index_in_turn<T>(i, lane)) : 0;
-    uint64_t left = __ballot(mask != 0);
-    while (left) {
-      const int from = __ffsll((unsigned long long)left) - 1;
-      left &= left - 1;
-      const uint64_t one = lane_key(key, from);
-      if (one > bar) {
-        list = insert(list, one, lane);
-        bar = lane_key(list, top - 1);
-      }
-    }
-    mask &= mask - 1;
-  }
-  return list;
 }
 
-// One row or a part of it to a workgroup; its waves take turns of 64 * kPer values,
-// which stay in registers between the search for the largest and the sums.
-template <typename T, bool TOP>
+// Without top tokens. One row or a part of it to a workgroup; its waves take turns of 64 *
+// PER values, which stay in registers between the search for the largest and the sums.
+template <typename T, int PER>
 __global__ __launch_bounds__(64 * kWaves) void logprobs(LogprobArgs a) {
   __shared__ Sums sums[kWaves];
-  __shared__ uint64_t keys[kWaves * 64];
-  __shared__ uint64_t best[64];
   __shared__ int last;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int row = blockIdx.x / a.parts, own = blockIdx.x % a.parts;
-  const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.ld_x;
+  const int64_t row = a.row0 + blockIdx.x / a.parts;
+  const int own = blockIdx.x % a.parts;
+  const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   const int from = (int)((int64_t)a.chunks * own / a.parts);
   const int to = (int)((int64_t)a.chunks * (own + 1) / a.parts);
   Sums t = {-INFINITY, 0.0f, 0.0f};
-  uint64_t list = 0;
   for (int chunk = from + wave; chunk < to; chunk += kWaves) {
-    float v[kPer];
-    load_turn(x, chunk * kTurn, a.n, lane, v);
-    float m = v[0];
-#pragma unroll
-    for (int i = 1; i < kPer; ++i) m = fmaxf(m, v[i]);
-    Sums u = {m, 0.0f, 0.0f};
-    const float r = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const float z = a.c * (v[i] - r), e = __builtin_amdgcn_exp2f(z);
-      u.s += e;
-      u.e = __builtin_fmaf(fmaxf(z, -1e4f), e, u.e);     // 0 where e is, z -infinity or not
-    }
-    t.add(u, a.c);
-    if (TOP) list = take_turn<T>(list, v, chunk * kTurn, chunk == from + wave, a.top, lane);
+    float v[PER];
+    load_turn<T, PER>(x, chunk * (64 * PER), a.n, lane, v);
+    t.add(sums_of<PER>(v, a.c), a.c);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const Sums o = {__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.e, d)};
-    t.add(o, a.c);
-  }
+  t.all(a.c);
   if (lane == 0) sums[wave] = t;
-  if (TOP) keys[threadIdx.x] = list;
   __syncthreads();
-  t = sums[0];
+  if (wave == 0) {
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) t.add(sums[w], a.c);
-  const int top = TOP ? a.top : 0;
-  if (TOP) {
-    // a key's place among the waves' first `top`
-    int place = lane < top && list ? 0 : 64;
-    for (int w = 0; w < kWaves; ++w)
-      for (int i = 0; i < top; ++i) place += keys[64 * w + i] > list;
-    if (threadIdx.x < 64) best[threadIdx.x] = 0;
-    __syncthreads();
-    if (place < top) best[place] = list;
-    __syncthreads();
+    for (int w = 1; w < kWaves; ++w) t.add(sums[w], a.c);
   }
   if (a.parts > 1) {
-    const int size = kPartFloats + 2 * top;
-    float* mine = a.part + (int64_t)blockIdx.x * size;
+    float* all = a.part + (int64_t)(row - a.row0) * a.parts * kPartFloats;
     if (threadIdx.x == 0) {
-      put_pair(mine, t.m, t.s);
-      put_pair(mine + 2, t.e, 0.0f);
+      put_pair(all + own * kPartFloats, t.m, t.s);
+      put_pair(all + own * kPartFloats + 2, t.e, 0.0f);
     }
-    if (TOP && threadIdx.x < top)
-      put_pair(mine + kPartFloats + 2 * threadIdx.x, bits_f32((uint32_t)best[threadIdx.x]),
-               bits_f32((uint32_t)(best[threadIdx.x] >> 32)));
-    if (!comes_last(a.count + row, a.parts, &last)) return;
-    const float* all = a.part + (int64_t)row * a.parts * size;
+    if (!comes_last(a.count + row - a.row0, a.parts, &last)) return;
     t = {-INFINITY, 0.0f, 0.0f};
-    for (int p = 0; p < a.parts; ++p) {
-      const f32x2 ms = get_pair(all + (int64_t)p * size), e = get_pair(all + (int64_t)p * size + 2);
-      t.add({ms[0], ms[1], e[0]}, a.c);
+    if (lane < a.parts) {
+      const f32x2 ms = get_pair(all + lane * kPartFloats), e = get_pair(all + lane * kPartFloats + 2);
+      t = {ms[0], ms[1], e[0]};
     }
-    if (TOP && wave == 0) {
-      list = best[lane];
-      for (int p = 0; p < a.parts; ++p) {
-        if (p == own) continue;
-        uint64_t key = 0;
-        if (lane < top) {
-          const f32x2 k = get_pair(all + (int64_t)p * size + kPartFloats + 2 * lane);
-          key = (uint64_t)f32_bits(k[1]) << 32 | f32_bits(k[0]);
-        }
-        for (int i = 0; i < top; ++i) {
-          const uint64_t one = lane_key(key, i);
-          if (one <= lane_key(list, top - 1)) break;
-          list = insert(list, one, lane);
-        }
-      }
-      best[lane] = list;
-    }
-    __syncthreads();
+    t.all(a.c);
   }
-  // a row of -infinity alone has no probability anywhere; with a NaN or an
-  // infinity in it (S is NaN) it has no distribution
-  const bool empty = t.s == 0.0f;
-  const float r = empty ? 0.0f : t.m, log = empty ? 0.0f : logf(t.s);
-  if (threadIdx.x == 0) {
-    if (a.entropy) a.entropy[row] = empty ? 0.0f : log - kLn2 * (t.e / t.s);
-    if (a.logprob) {
-      const int token = a.tokens[row];
-      float p = 0.0f;
-      if (token >= a.n) p = bits_f32(0x7FC00000u);
-      else if (token >= 0) p = a.scale * ((float)x[token] - r) - log;
-      a.logprob[row] = p;
-    }
+  if (threadIdx.x == 0) finish(a, row, x, t);
+}
+
+// A bar that k of 256 maxima reach and few more, by its bits from the top: the k-th
+// largest one at most. Every wave finds it for itself.
+__device__ __forceinline__ uint32_t bar_of(const uint32_t* maxima, int k, int lane) {
+  uint32_t g[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) g[q] = maxima[64 * q + lane];
+  // the bits that all of them share come first
+  uint32_t high = max(max(g[0], g[1]), max(g[2], g[3])), low = min(min(g[0], g[1]), min(g[2], g[3]));
+  high = max(high, lane_xor<1>(high)), low = min(low, lane_xor<1>(low));
+  high = max(high, lane_xor<2>(high)), low = min(low, lane_xor<2>(low));
+  high = max(high, lane_xor<4>(high)), low = min(low, lane_xor<4>(low));
+  high = max(high, lane_xor<8>(high)), low = min(low, lane_xor<8>(low));
+  high = max(high, lane_xor<16>(high)), low = min(low, lane_xor<16>(low));
+  high = max(high, lane_xor<32>(high)), low = min(low, lane_xor<32>(low));
+  high = __builtin_amdgcn_readfirstlane(high), low = __builtin_amdgcn_readfirstlane(low);
+  if (high == low) return high;
+  const int first = 31 - __builtin_clz(high ^ low);
+  uint32_t bar = high & ~((2u << first) - 1);
+  for (uint32_t bit = 1u << first; bit; bit >>= 1) {
+    const uint32_t up = bar | bit;
+    int reach = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) reach += __popcll(__ballot(g[q] >= up));
+    if (reach >= k) bar = up;
+    if (reach >= k && reach <= k + kMore) break;
   }
-  if (TOP && threadIdx.x < top) {
-    const uint64_t key = best[threadIdx.x];
-    const bool none = t.s != t.s;
-    a.top_logprobs[row * a.ld_top + threadIdx.x] =
-        none ? bits_f32(0x7FC00000u) : a.scale * (value_of(key) - r) - log;
-    a.top_tokens[row * a.ld_top + threadIdx.x] = none ? -1 : index_of(key);
+  return bar;
+}
+
+// Room in the list for the lanes of `some`; a lane's place.
+__device__ __forceinline__ int places(int* count, uint64_t some, int lane) {
+  int first = 0;
+  if (lane == 0) first = atomicAdd(count, (int)__popcll(some));
+  return __builtin_amdgcn_readfirstlane(first) + (int)__popcll(some & ((1ull << lane) - 1));
+}
+
+// Each key of a list at its place among the first k; a list of fewer leaves zeros. The list
+// has kRankRun - 1 keys of 0 behind it.
+constexpr int kRankRun = 8;
+__device__ __forceinline__ void rank(const uint64_t* list, int count, int k, uint64_t* best) {
+  for (int i = threadIdx.x; i < count; i += blockDim.x) {
+    const uint64_t key = list[i];
+    int place = 0;
+    for (int j = 0; j < count; j += kRankRun) {
+      uint64_t some[kRankRun];
+#pragma unroll
+      for (int q = 0; q < kRankRun; ++q) some[q] = list[j + q];
+#pragma unroll
+      for (int q = 0; q < kRankRun; ++q) place += some[q] > key;
+    }
+    if (place < k) best[place] = key;
   }
 }
 
-int32_t parts_of(int64_t rows, int64_t n) {
-  const int64_t chunks = (n + kTurn - 1) / kTurn;
-  // a few workgroups for each CU, and a turn for each wave at least
-  const int64_t most = std::min<int64_t>(1024 / std::max<int64_t>(rows, 1), 64);
-  return (int32_t)std::max<int64_t>(1, std::min(most, chunks / kWaves));
+// With top tokens. Every wave takes one turn, so that its values stay in registers until
+// the bar is known. Values above the bar are in k + kMore groups at most (where
+// more maxima reach it, it is the k-th largest); of those equal to it a wave needs the
+// k first ones only.
+template <typename T, int PER, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 8 : 4) void logprobs_top(LogprobArgs a) {
+  constexpr int LANES = WAVES / 4;               // of a group
+  constexpr int ABOVE = (64 + kMore) * LANES * PER;
+  constexpr int LIST = std::max(ABOVE + 64 * WAVES, 64 * kMostParts);
+  __shared__ Sums sums[WAVES];
+  __shared__ uint32_t maxima[256];
+  __shared__ uint64_t list[LIST + kRankRun], best[64];
+  __shared__ int count, last;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row = a.row0 + blockIdx.x / a.parts;
+  const int own = blockIdx.x % a.parts, k = a.top;
+  const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+  const int base = (own * WAVES + wave) * (64 * PER);
+  float v[PER];
+  load_turn<T, PER>(x, base, a.n, lane, v);
+  Sums t = sums_of<PER>(v, a.c);
+  uint32_t most = order_of(t.m);
+  if (LANES >= 2) most = max(most, lane_xor<1>(most));
+  if (LANES >= 4) most = max(most, lane_xor<2>(most));
+  if (lane % LANES == 0) maxima[threadIdx.x / LANES] = most;
+  if (threadIdx.x < 64) best[threadIdx.x] = 0;
+  if (threadIdx.x == 0) count = 0;
+  t.all(a.c);
+  if (lane == 0) sums[wave] = t;
+  __syncthreads();
+  {
+    const float bar = value_of(bar_of(maxima, k, lane));
+    uint32_t above = 0, equal = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      above |= v[i] > bar ? 1u << i : 0;
+      equal |= v[i] == bar ? 1u << i : 0;
+    }
+    int ties = __popc(equal);
+    ties += lane_xor<1>((uint32_t)ties);
+    ties += lane_xor<2>((uint32_t)ties);
+    ties += lane_xor<4>((uint32_t)ties);
+    ties += lane_xor<8>((uint32_t)ties);
+    ties += lane_xor<16>((uint32_t)ties);
+    ties += lane_xor<32>((uint32_t)ties);
+    if (__builtin_amdgcn_readfirstlane(ties) <= 64) {
+      above |= equal;
+    } else {
+      // in the order of their indices: run by run, lane by lane
+      constexpr int W = kRun<T>;
+      int taken = 0;
+      for (int i = 0; i < PER && taken < k; i += W) {
+        const uint32_t bits = equal >> i & ((1u << W) - 1);
+        int before = taken, all = 0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const uint64_t with = __ballot(bits >> j & 1);
+          before += __popcll(with & ((1ull << lane) - 1));
+          all += __popcll(with);
+        }
+        for (int j = 0; j < W; ++j) {
+          const bool mine = (bits >> j & 1) && before < k;
+          const uint64_t some = __ballot(mine);
+          if (!some) continue;
+          const int place = places(&count, some, lane);
+          if (mine) list[place] = key_of(bar, base + index_in_turn<T>(i, lane) + j);
+          before += bits >> j & 1;
+        }
+        taken += all;
+      }
+    }
+    while (const uint64_t some = __ballot(above != 0)) {
+      const int i = above ? __ffs(above) - 1 : 0;
+      float one = v[0];
+#pragma unroll
+      for (int j = 1; j < PER; ++j) one = i == j ? v[j] : one;
+      const int place = places(&count, some, lane);
+      if (above) list[place] = key_of(one, base + index_in_turn<T>(i, lane));
+      above &= above - 1;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < kRankRun) list[count + threadIdx.x] = 0;
+  __syncthreads();
+  rank(list, count, k, best);
+  if (wave == 0) {
+    t = {-INFINITY, 0.0f, 0.0f};
+    if (lane < WAVES) t = sums[lane];
+    t.all(a.c);
+  }
+  __syncthreads();
+  if (a.parts > 1) {
+    const int size = kPartFloats + 2 * k;
+    float* all = a.part + (int64_t)(row - a.row0) * a.parts * size;
+    if (wave == 0) {
+      float* mine = all + (int64_t)own * size;
+      if (lane == 0) put_pair(mine, t.m, t.s);
+      if (lane == 1) put_pair(mine + 2, t.e, 0.0f);
+      if (lane < k)
+        put_pair(mine + kPartFloats + 2 * lane, bits_f32((uint32_t)best[lane]),
+                 bits_f32((uint32_t)(best[lane] >> 32)));
+    }
+    if (!comes_last(a.count + row - a.row0, a.parts, &last)) return;
+    // the parts' keys, a part to a wave at a time, and the same again
+    constexpr int EACH = kMostParts / WAVES;
+    f32x2 both[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)                 // all on their way before one is looked at
+      both[i] = get_pair(all + (int64_t)min(i * WAVES + wave, a.parts - 1) * size + kPartFloats +
+                         2 * min(lane, k - 1));
+    uint64_t keys[EACH];
+    most = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const bool here = i * WAVES + wave < a.parts && lane < k;
+      keys[i] = here ? (uint64_t)f32_bits(both[i][1]) << 32 | f32_bits(both[i][0]) : 0;
+      most = max(most, (uint32_t)(keys[i] >> 32));
+    }
+    if (LANES >= 2) most = max(most, lane_xor<1>(most));
+    if (LANES >= 4) most = max(most, lane_xor<2>(most));
+    if (lane % LANES == 0) maxima[threadIdx.x / LANES] = most;
+    if (threadIdx.x < 64) best[threadIdx.x] = 0;
+    if (threadIdx.x == 0) count = 0;
+    if (wave == 0) {
+      t = {-INFINITY, 0.0f, 0.0f};
+      if (lane < a.parts) {
+        const f32x2 ms = get_pair(all + (int64_t)lane * size);
+        const f32x2 e = get_pair(all + (int64_t)lane * size + 2);
+        t = {ms[0], ms[1], e[0]};
+      }
+      t.all(a.c);
+    }
+    __syncthreads();
+    const uint32_t bar = bar_of(maxima, k, lane);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const bool mine = keys[i] && (uint32_t)(keys[i] >> 32) >= bar;
+      const uint64_t some = __ballot(mine);
+      if (!some) continue;
+      const int place = places(&count, some, lane);
+      if (mine) list[place] = keys[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < kRankRun) list[count + threadIdx.x] = 0;
+    __syncthreads();
+    rank(list, count, k, best);
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  if (lane == 0) finish(a, row, x, t);
+  if (lane < k) {
+    const Row f(t);
+    const uint64_t key = best[lane];
+    a.top_logprobs[row * a.ld_top + lane] =
+        f.none ? bits_f32(0x7FC00000u) : f.logprob(value_of((uint32_t)(key >> 32)), a.scale);
+    a.top_tokens[row * a.ld_top + lane] = f.none ? -1 : index_of(key);
+  }
+}
+
+constexpr int kPer = 32;
+
+// How a call is split: rows over launches, since there are 16384 counters of parts,
+// and each row over workgroups.
+struct Plan {
+  bool wide;                     // with top tokens: 16 waves of 32 values a lane, or 4 of 16
+  int32_t parts;
+  int64_t rows;                  // of a launch
+};
+
+Plan plan_of(const ifq_logprobs_desc& d) {
+  Plan p = {false, 1, d.rows};
+  if (d.top) {
+    // us, narrow and wide (bfloat16, 10 top tokens): 1 x 16000 8.4 and 8.4, 256 x 16000 13.2
+    // and 11.3, 4000 x 16000 129 and 88, 1 x 50000 9.4 and 16.7, 64 x 50000 14.7 and 18.5,
+    // 64 x 128000 27 and 16, 1000 x 128000 269 and 113; but 1000 x 8000 22 and 26
+    const int64_t narrow = (d.n + 4095) / 4096;
+    p.wide = d.n > 8192 && (d.n <= 32768 || narrow * d.rows > 1536 || narrow > kMostParts);
+    p.parts = (int32_t)(p.wide ? (d.n + 32767) / 32768 : narrow);
+  } else {
+    // a few workgroups for each CU, and a turn for each wave at least
+    const int64_t turns = (d.n + 64 * kPer - 1) / (64 * kPer);
+    const int64_t most = std::min<int64_t>(1024 / std::max<int64_t>(d.rows, 1), 64);
+    p.parts = (int32_t)std::max<int64_t>(1, std::min(most, turns / kWaves));
+  }
+  const int64_t counters = kSplitCounterBytes / (int64_t)sizeof(uint32_t);
+  if (p.parts > 1) p.rows = std::min(p.rows, counters);
+  return p;
 }
 
 }  // namespace
 
 size_t logprobs_workspace_bytes(const ifq_logprobs_desc& d) {
   if (d.rows == 0) return 0;
-  const int64_t parts = parts_of(d.rows, d.n);
-  if (parts == 1) return 0;
-  return kSplitCounterBytes + d.rows * parts * (kPartFloats + 2 * d.top) * sizeof(float);
+  const Plan p = plan_of(d);
+  if (p.parts == 1) return 0;
+  return kSplitCounterBytes + p.rows * p.parts * (kPartFloats + 2 * d.top) * sizeof(float);
 }
 
-int64_t logprobs_groups(const ifq_logprobs_desc& d) { return d.rows * parts_of(d.rows, d.n); }
+int64_t logprobs_groups(const ifq_logprobs_desc& d) {
+  const Plan p = plan_of(d);
+  return p.rows * p.parts * (p.wide ? 4 : 1);
+}
 
 hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const int32_t* tokens,
                            float* logprob, float* entropy, float* top_logprobs,
                            int32_t* top_tokens, void* ws, hipStream_t stream) {
+  const Plan p = plan_of(d);
   LogprobArgs a;
   a.x = logits;
   a.tokens = tokens;
@@ -327,20 +524,28 @@ hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const
   a.ld_top = d.ld_top;
   a.n = (int32_t)d.n;
   a.top = d.top;
-  a.parts = parts_of(d.rows, d.n);
-  a.chunks = (int32_t)((d.n + kTurn - 1) / kTurn);
+  a.parts = p.parts;
+  a.chunks = (int32_t)((d.n + 64 * kPer - 1) / (64 * kPer));
   a.scale = d.scale;
   a.c = d.scale * 1.4426950408889634f;
-  const dim3 grid((uint32_t)logprobs_groups(d)), block(64 * kWaves);
-  auto go = [&](auto zero) {
-    typedef decltype(zero) T;
-    if (d.top) hipLaunchKernelGGL((logprobs<T, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((logprobs<T, false>), grid, block, 0, stream, a);
-  };
-  if (d.x_type == IFQ_TYPE_BF16) go(__bf16(0));
-  else if (d.x_type == IFQ_TYPE_F16) go(_Float16(0));
-  else go(0.0f);
-  return hipGetLastError();
+  for (int64_t row = 0; row < d.rows; row += p.rows) {
+    a.row0 = row;
+    const dim3 grid((uint32_t)(std::min(p.rows, d.rows - row) * p.parts));
+    auto go = [&](auto zero) {
+      typedef decltype(zero) T;
+      if (!d.top)
+        hipLaunchKernelGGL((logprobs<T, kPer>), grid, dim3(64 * kWaves), 0, stream, a);
+      else if (p.wide)
+        hipLaunchKernelGGL((logprobs_top<T, 32, 16>), grid, dim3(1024), 0, stream, a);
+      else
+        hipLaunchKernelGGL((logprobs_top<T, 16, 4>), grid, dim3(256), 0, stream, a);
+    };
+    if (d.x_type == IFQ_TYPE_BF16) go(__bf16(0));
+    else if (d.x_type == IFQ_TYPE_F16) go(_Float16(0));
+    else go(0.0f);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ifq

@@ -220,6 +220,8 @@ ifq_status check_logprobs(const ifq_logprobs_desc* d) {
     return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: reserved must be 0");
   if (d->ld_x < d->n || d->ld_top < d->top || d->ld_x > kMaxStride || d->ld_top > kMaxStride)
     return fail(IFQ_ERR_INVALID_ARGUMENT, "logprobs: a leading dimension is below its row");
+  if (d->top > 0 && d->n > ifq::kMostTopValues)
+    return fail(IFQ_ERR_UNSUPPORTED, "logprobs: top tokens of up to 2^20 values");
   if (ifq::logprobs_groups(*d) > ifq::kMaxGroups)
     return fail(IFQ_ERR_UNSUPPORTED, "logprobs: too many rows for one launch");
   return IFQ_OK;

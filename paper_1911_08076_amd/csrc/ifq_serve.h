@@ -60,8 +60,9 @@ hipError_t launch_f4_matmul(const ifq_f4_matmul_desc& d, const void* x, const vo
                             const void* gate_scales, const void* w, const void* w_scales,
                             void* y, void* ws, hipStream_t stream);
 
+constexpr int64_t kMostTopValues = 1 << 20;     // of a row, with top tokens: 32 parts of 32768
 size_t logprobs_workspace_bytes(const ifq_logprobs_desc& d);
-int64_t logprobs_groups(const ifq_logprobs_desc& d);
+int64_t logprobs_groups(const ifq_logprobs_desc& d);   // threads of a launch, in workgroups of 256
 hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const int32_t* tokens,
                            float* logprob, float* entropy, float* top_logprobs,
                            int32_t* top_tokens, void* ws, hipStream_t stream);

@@ -97,7 +97,7 @@ def test_products_refuse_pointers():
     (dict(scale=-1.0), EINVAL), (dict(scale=float("nan")), EINVAL),
     (dict(scale=float("inf")), EINVAL), (dict(scale=2.0 ** 65), EINVAL),
     (dict(reserved=1), EINVAL), (dict(ld_x=99), EINVAL), (dict(ld_top=4), EINVAL),
-    (dict(rows=2 ** 30), EUNSUP)])
+    (dict(rows=2 ** 30), EUNSUP), (dict(n=2 ** 20 + 1, ld_x=2 ** 21), EUNSUP)])
 def test_logprobs_refuses_descriptors(change, status):
     d = changed(P.logprobs_desc(8, 100, BF16, top=5), change)
     refused(status, P.ifq_logprobs, d, X, X, X, X, X, X)

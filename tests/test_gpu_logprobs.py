@@ -72,6 +72,34 @@ def test_logprobs_many_rows(kind, rng):
     check(logits(rng, 3000, 401, kind), rng.integers(0, 401, 3000).tolist(), 4)
 
 
+def test_logprobs_more_rows_than_counters(rng):
+    """Rows in two parts each, more of them than a launch takes."""
+    check(logits(rng, 17001, 4100, "bf16"), rng.integers(0, 4100, 17001).tolist(), 2)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,top", [
+    (1, 4096, 64), (1, 4097, 64), (3, 8192, 20), (2, 8193, 64), (2, 32768, 33), (1, 32769, 64),
+    (1, 131072, 64), (1, 131073, 64), (40, 131072, 5), (60, 131071, 5), (1, 1048576, 64)])
+def test_logprobs_splits(kind, rows, n, top, rng):
+    """At either side of each change of the split."""
+    check(logits(rng, rows, n, kind), rng.integers(0, n, rows).tolist(), top)
+
+
+@pytest.mark.parametrize("n,top", [(4000, 64), (30000, 64), (60000, 40), (100000, 3)])
+def test_logprobs_best_in_one_place(n, top, rng):
+    """The top tokens all in a few lanes, or all equal and everywhere."""
+    x = logits(rng, 6, n, "f32", 0.01)
+    x[0, n // 2:n // 2 + 100] += 50
+    x[1, :200] = torch.arange(200, device=DEV) + 50.0
+    x[2, -200:] = -torch.arange(200, device=DEV) + 300.0
+    x[3, ::3] = 7.0
+    x[4, n // 3:] = -torch.inf
+    x[5] = torch.arange(n, device=DEV) % 4 * 1.0
+    for kind in TYPES:
+        check(x.to(TYPES[kind][0]), [0] * 6, top)
+
+
 @pytest.mark.parametrize("n", [100, 3000, 40000])
 @pytest.mark.parametrize("top", [0, 9])
 def test_logprobs_outputs_left_out(n, top, rng):
