@@ -7,7 +7,9 @@ on codes (Eq. 4), and a layer-chain driver. All of it lives in libifq.so
 (HIP for gfx950 plus host C++); this package is its Python binding. Beside it,
 operators for serving language models in low-bit codes: 8-bit float products
 with a scale per block of 128, a paged cache of keys and values in 4-bit codes
-and attention over it (AttentionLayer runs them together).
+and attention over it (AttentionLayer runs them together), products with weights
+in 4-bit floats, a gated feed-forward block of them (FeedForward) and log
+probabilities of tokens (Classifier).
 
 Importing the package loads libifq.so and raises ImportError if it has not
 been built: there is no CPU fallback.
@@ -20,6 +22,8 @@ from .api import *  # noqa: E402,F401,F403
 from .api import IfqError  # noqa: E402,F401
 from .stack import DeviceStack, conv_ops  # noqa: E402,F401
 from .attention import AttentionLayer, F8Linear, rotation_tables  # noqa: E402,F401
+from .feed_forward import (Classifier, F4Linear, F4Weight, FeedForward,  # noqa: E402,F401
+                           TokenLogprobs, token_logprobs)
 from ._ffi import (IFQ_LAYOUT_I8_NHWC, IFQ_LAYOUT_U2_NHWC_PACKED,  # noqa: E402,F401
                    IFQ_LAYOUT_I32_NHWC, IFQ_LAYOUT_U2_BLOCK64, IFQ_POOL_VALID, IFQ_POOL_SAME,
                    IFQ_JOIN_NONE, IFQ_JOIN_IDENTITY, IFQ_JOIN_CONV,

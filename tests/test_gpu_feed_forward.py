@@ -1,0 +1,197 @@
+"""The feed-forward layers on the GPU: they are their calls, and what the weights
+stand for; a decoder layer of attention, feed-forward block and classifier, eager
+and captured; prompts and single tokens."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+import paper_1911_08076_amd as P
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def randn(g, *shape, scale=1.0, dtype=torch.bfloat16):
+    return (torch.randn(*shape, generator=g, device=DEV) * scale).to(dtype)
+
+
+def make(hidden=272, inner=700, vocabulary=1001, dtype=torch.bfloat16):
+    g = torch.Generator(device=DEV).manual_seed(5)
+    feed = P.FeedForward(randn(g, inner, hidden, scale=hidden ** -0.5, dtype=dtype),
+                         randn(g, inner, hidden, scale=hidden ** -0.5, dtype=dtype),
+                         randn(g, hidden, inner, scale=inner ** -0.5, dtype=dtype))
+    head = P.Classifier(randn(g, vocabulary, hidden, scale=3 * hidden ** -0.5, dtype=dtype))
+    return feed, head, g
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m", [1, 5, 40, 300])
+def test_block_is_what_its_weights_stand_for(m, dtype):
+    """In 64 bits with the inner values rounded to the type: an inner value's product with its
+    gate is off by its rounding u, and a rounding of an inner value beside the oracle's by another;
+    sums in fp32 add a few 2^-24 of their terms' magnitudes."""
+    feed, _, g = make(dtype=dtype)
+    x = randn(g, m, 272, dtype=dtype)
+    u = torch.finfo(dtype).eps / 2
+    gate, up, down = (w.values().double() for w in (feed.gate, feed.up, feed.down.weight))
+    a, b = x.double() @ gate.T, x.double() @ up.T
+    inner = a / (1 + torch.exp(-a)) * b
+    want = inner @ down.T
+    size = inner.abs() @ down.abs().T
+    # what sums of 272 terms in fp32 may be off by, in the gate (whose slope is below 1.1) and beside it
+    far = 300 * 2.0 ** -23 * (1.1 * (x.double().abs() @ gate.abs().T) * b.abs() +
+                              (x.double().abs() @ up.abs().T) * a.abs()) + 32 * 2.0 ** -23 * inner.abs()
+    bound = (far * (1 + u)) @ down.abs().T + u * size + 720 * 2.0 ** -23 * size
+    bound += u * (want.abs() + bound) + 2.0 ** -24
+    assert ((feed(x).double() - want).abs() <= bound).all()
+
+
+def test_linear_types_and_outputs():
+    g = torch.Generator(device=DEV).manual_seed(6)
+    lin = P.F4Linear(randn(g, 100, 272, dtype=torch.float32))
+    x = randn(g, 7, 272)
+    y = lin(x)
+    assert y.dtype == torch.bfloat16 and torch.equal(lin(x, dtype=torch.float32).to(y.dtype), y)
+    out = torch.empty(7, 100, device=DEV)
+    assert lin(x, out=out) is out and torch.equal(out.to(y.dtype), y)
+    assert lin(x[:0]).shape == (0, 100)
+    w = lin.weight.values()
+    assert torch.equal(P.F4Weight(w).codes, lin.weight.codes)     # a code's own value keeps it
+
+
+def test_logprobs_of_the_classifier():
+    feed, head, g = make()
+    x = randn(g, 9, 272)
+    tokens = i32([0, 5, 1000, -1, 3, 7, 9, 11, 13])
+    got = head(x, tokens, top=3, scale=0.5)
+    logits = head.linear(x, dtype=torch.float32)
+    same = P.token_logprobs(logits, tokens, 3, 0.5)
+    assert all(torch.equal(a, b) for a, b in zip(got, same))
+    p = torch.log_softmax(0.5 * logits.double(), 1)
+    assert torch.allclose(got.logprob[[0, 1, 2]].double(), p[[0, 1, 2], [0, 5, 1000]], atol=1e-5)
+    assert got.logprob[3] == 0 and torch.equal(got.top_tokens[:, 0].long(), logits.argmax(1))
+    assert torch.allclose(got.entropy.double(), -(p.exp() * p).sum(1), atol=1e-5)
+    none = head(x, top=0)
+    assert none.logprob is None and none.top_tokens is None and torch.equal(none.entropy,
+                                                                            head(x, top=0).entropy)
+
+
+class Decoder:
+    """One layer, and the tokens it answers with."""
+
+    def __init__(self, hidden=272, vocabulary=40000):
+        self.feed, self.head, g = make(hidden, 700, vocabulary)
+        self.attention = P.AttentionLayer(
+            randn(g, (4 + 2 * 2) * 64, hidden, scale=hidden ** -0.5),
+            randn(g, hidden, 4 * 64, scale=256 ** -0.5), 4, 2, 64, num_pages=12, max_pages=4,
+            page_tokens=32)
+        self.embedding = randn(g, vocabulary, hidden)
+        self.g = g
+
+    def __call__(self, tokens, offsets, lengths, pages, max_q, given=None, top=5):
+        x = self.embedding[tokens]
+        x = x + self.attention(x, offsets, lengths, pages, max_q=max_q)
+        x = x + self.feed(x)
+        return self.head(x, given, top=top)
+
+
+def test_decoder_step_captured():
+    """A captured step over a growing sequence gives the eager steps' bits; eager prompts and a
+    second captured graph on the same workspaces in between leave it alone."""
+    d = Decoder()
+    prompt = torch.randint(0, 40000, (50,), generator=d.g, device=DEV, dtype=torch.int32)
+    pages, other = i32([[3, 1, 0, 2]]), i32([[7, 5, 4, 6]])
+
+    def eager(cache_pages, first, steps):
+        token = prompt[:1].clone()
+        said = []
+        for i in range(first, first + steps):
+            a = d(token, i32([0, 1]), i32([i + 1]), cache_pages, 1, given=token)
+            said.append([t.clone() for t in a])
+            token = a.top_tokens[:, 0].contiguous()
+        return said
+
+    d(prompt, i32([0, 50]), i32([50]), pages, 50)
+    want = eager(pages, 50, 15)
+    d.attention.cache.zero_()
+    d(prompt, i32([0, 50]), i32([50]), pages, 50)
+    token, offs, lens = prompt[:1].clone(), i32([0, 1]), i32([50])
+    two = (prompt[:2].clone(), i32([0, 2]), i32([2]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        d(token, offs, i32([1]), other, 1, given=token)
+        d(two[0], two[1], two[2], other, 2)
+    torch.cuda.current_stream().wait_stream(side)
+    graph, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lens.add_(1)
+        out = d(token, offs, lens, pages, 1, given=token)
+        token.copy_(out.top_tokens[:, 0])
+    with torch.cuda.graph(second):
+        out2 = d(two[0], two[1], two[2], other, 2)
+    want2 = None
+    for i, w in enumerate(want):
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(out, w)), i
+        second.replay()
+        if want2 is None:
+            want2 = [t.clone() for t in d(two[0], two[1], two[2], other, 2) if t is not None]
+        assert all(torch.equal(a, b) for a, b in zip((t for t in out2 if t is not None), want2))
+        if i % 4 == 1:
+            d(prompt, i32([0, 50]), i32([50]), other, 50)
+            torch.cuda.synchronize()
+
+
+def test_prompt_and_single_tokens_agree():
+    """Scores of a prompt at once and token by token: the codes of the attention may come out
+    beside one another (some hundredths of its output), and the logits with them."""
+    d = Decoder(vocabulary=3000)
+    prompt = torch.randint(0, 3000, (60,), generator=d.g, device=DEV, dtype=torch.int32)
+    given = torch.cat([prompt[1:], i32([-1])])
+    pages = i32([[3, 1, 0, 2]])
+    whole = d(prompt, i32([0, 60]), i32([60]), pages, 60, given)
+    d.attention.cache.zero_()
+    ones = [d(prompt[i:i + 1].contiguous(), i32([0, 1]), i32([i + 1]), pages, 1,
+              given[i:i + 1].contiguous()) for i in range(60)]
+    a, b = torch.cat([o.logprob for o in ones]), whole.logprob
+    assert b[59] == 0 and (a - b).abs().max() < 0.1 * b.abs().max()
+    assert (torch.cat([o.top_tokens[:, 0] for o in ones]) == whole.top_tokens[:, 0]).float().mean() > 0.8
+
+
+def test_calls_on_another_stream():
+    feed, head, g = make(vocabulary=50001)
+    x = randn(g, 3, 272)
+    want = head(feed(x), top=4)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        got = head(feed(x), top=4)
+    st.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got[1:], want[1:]))
+    logits = head.linear(x, dtype=torch.float32)
+    d = P.logprobs_desc(3, 50001, P.IFQ_TYPE_F32, 4)
+    h, best, at = torch.empty(3, device=DEV), torch.empty(3, 4, device=DEV), torch.empty(
+        3, 4, dtype=torch.int32, device=DEV)
+    st.wait_stream(torch.cuda.current_stream())
+    P.ifq_logprobs(d, logits, None, None, h, best, at, stream=st)   # makes its own workspace
+    st.synchronize()
+    same = P.token_logprobs(logits, top=4)
+    assert torch.equal(h, same.entropy) and torch.equal(at, same.top_tokens)
+
+
+def test_example_runs(capsys):
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "decode.py")
+    spec = importlib.util.spec_from_file_location("decode_example", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    mod.main(["--batch", "3", "--prompt", "150", "--tokens", "12", "--vocabulary", "2000"])
+    said = capsys.readouterr().out
+    assert "tokens scored" in said and "decoding: 3 sequences" in said
