@@ -36,6 +36,12 @@ def _output(x, n, dtype, out):
     return out
 
 
+def _overlap(a, b):
+    """Dense tensors that share memory."""
+    return (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size() and
+            b.data_ptr() < a.data_ptr() + a.numel() * a.element_size())
+
+
 class F4Weight:
     """Weights [out][in] as codes and scales (ifq_f4_quantize)."""
 
@@ -71,11 +77,18 @@ class F4Linear:
         self.workspace = _Workspace() if workspace is None else workspace
 
     def __call__(self, x, out=None, dtype=None):
-        """x [m][in] -> [m][out] of dtype (None: out's, or x's)."""
+        """x [m][in] -> [m][out] of dtype (None: out's, or x's). out must not overlap x."""
         w = self.weight
         dev = w.codes.device
         _check_rows(x, w.k, _HALVES, dev)
-        out = _output(x, w.n, dtype, out)
+        y = _output(x, w.n, dtype, out)
+        if out is not None and _overlap(x, out):
+            raise ValueError("an output that overlaps the input")
+        return self._product(x, y)
+
+    def _product(self, x, out):
+        w = self.weight
+        dev = w.codes.device
         if x.shape[0]:
             with _on(dev):
                 d = P.f4_matmul_desc(x.shape[0], w.n, w.k, _TYPES[x.dtype], _TYPES[out.dtype])
@@ -104,7 +117,7 @@ class FeedForward:
         self.down = F4Linear(weight_down, self.workspace)
 
     def __call__(self, x, out=None):
-        """x [m][hidden] (bfloat16 or float16) -> [m][hidden]."""
+        """x [m][hidden] (bfloat16 or float16) -> [m][hidden]; out may be x."""
         gate, up = self.gate, self.up
         dev = gate.codes.device
         _check_rows(x, gate.k, _HALVES, dev)
@@ -116,7 +129,7 @@ class FeedForward:
                                      activation=self.activation)
                 P.ifq_f4_gated(d, x, gate.codes, gate.scales, up.codes, up.scales, inner,
                                ws=self.workspace.get(P.ifq_f4_gated_workspace_bytes(d), dev))
-                self.down(inner, out=out)
+                self.down._product(inner, out)
         return out
 
 

@@ -97,6 +97,22 @@ def test_outputs_that_do_not_fit_are_refused(launches, out):
         F.F4Linear(empty(96, 64))(empty(3, 64), out=empty(3, 96), dtype=F32)
 
 
+def test_an_output_over_the_input_is_refused(launches, monkeypatch):
+    monkeypatch.setattr(F, "_overlap", lambda a, b: a is b)     # these have no addresses
+    layer, x = F.F4Linear(empty(64, 64)), empty(3, 64)
+    launches.seen.clear()
+    with pytest.raises(ValueError):
+        layer(x, out=x)
+    assert launches.seen == []
+
+
+def test_overlaps():
+    rows = torch.empty(8, 64, dtype=BF16)
+    assert F._overlap(rows, rows) and F._overlap(rows[:3], rows[2:5]) and F._overlap(rows[2:5], rows)
+    assert not F._overlap(rows[:3], rows[3:]) and not F._overlap(rows[3:], rows[:3])
+    assert not F._overlap(rows, torch.empty_like(rows)) and not F._overlap(rows[:0], rows)
+
+
 def test_logits_and_tokens_that_do_not_fit_are_refused(launches):
     good = empty(3, 50, dtype=F32)
     for x in (empty(3, 50, dev="cpu"), empty(50), empty(50, 3).t(), empty(3, 50, dtype=torch.int32)):

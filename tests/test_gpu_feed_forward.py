@@ -65,6 +65,25 @@ def test_linear_types_and_outputs():
     assert torch.equal(P.F4Weight(w).codes, lin.weight.codes)     # a code's own value keeps it
 
 
+def test_outputs_in_the_inputs_memory():
+    """A block may write over its input, a product only beside it."""
+    feed, _, g = make()
+    rows = randn(g, 80, 272)
+    want = feed(rows[:40])
+    x = rows.clone()
+    assert feed(x[:40], out=x[:40]).data_ptr() == x.data_ptr() and torch.equal(x[:40], want)
+    x = rows.clone()
+    feed(x[:40], out=x[20:60])
+    assert torch.equal(x[20:60], want) and torch.equal(x[:20], rows[:20]) and torch.equal(
+        x[60:], rows[60:])
+    lin = P.F4Linear(randn(g, 272, 272))
+    x = rows.clone()
+    want = lin(x[:40])
+    assert torch.equal(lin(x[:40], out=x[40:]), want) and torch.equal(x[:40], rows[:40])
+    with pytest.raises(ValueError):
+        lin(x[:40], out=x[39:79])
+
+
 def test_logprobs_of_the_classifier():
     feed, head, g = make()
     x = randn(g, 9, 272)
