@@ -978,7 +978,8 @@ IFQ_API const char* ifq_f4_gated_kernel_name(const ifq_f4_matmul_desc* d);
  *   y[i][j] = sum over k of x[i][k] * w[j][k]
  * with w the values that codes and scales stand for in x's type (float16: rounded
  * where they are below 2^-24 or above 65504), sums in fp32, rounded once to y's type.
- * Codes of columns past k and scales of groups past k may be anything.
+ * Codes of columns past k may be any that are finite in x's type (the quantizer's are 0),
+ * scales of groups past k anything.
  *   x          device [m][ld_x], aligned to its element
  *   w          device codes [n][ld_w], 16-byte aligned
  *   w_scales   device uint8 [ceil(k/128)][n][4], 4-byte aligned

@@ -108,6 +108,24 @@ def test_quantize_many_rows(rng):
     assert np.array_equal(scales[:, some].cpu().numpy(), ws)
 
 
+def test_quantize_rows_far_apart(rng):
+    """Offsets past 32 bits, of elements and of bytes."""
+    rows, k, ld_x, ld_codes = 1100, 70, 1 << 22, 1 << 22
+    x = torch.empty(rows, ld_x, dtype=torch.bfloat16, device=DEV)
+    x[:, :k] = torch.from_numpy(rng.standard_normal((rows, k))).to(x)
+    codes = torch.empty(rows, ld_codes, dtype=torch.uint8, device=DEV)
+    scales = torch.empty(1, rows, 4, dtype=torch.uint8, device=DEV)
+    d = P.f4_weights_desc(rows, k, P.IFQ_TYPE_BF16, ld_x, ld_codes)
+    P.ifq_f4_quantize(d, x, codes, scales)
+    want, ws = O.quantize(x[:, :k].double().cpu().numpy())
+    assert np.array_equal(codes[:, :48].cpu().numpy(), O.pack(want))
+    assert np.array_equal(scales.cpu().numpy(), ws)
+    x.fill_(-7)
+    P.ifq_f4_dequantize(d, codes, scales, x)
+    assert np.array_equal(x[:, :k].double().cpu().numpy(), O.values(want, ws, k))
+    assert (x[:, k] == -7).all()
+
+
 # -- products ----------------------------------------------------------------------
 class Weights:
     """Random codes; what ends past k holds anything."""
@@ -219,6 +237,42 @@ def test_product_values_at_the_ends_of_the_range(m, n, rng):
                 held = torch.from_numpy(held).float().half().double().numpy()
             assert np.isfinite(held).all()
             assert np.array_equal(got, rounded(h @ held.T, "f32")), (kind, byte)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 70, 1), (3, 70, 100), (20, 100, 287), (70, 100, 33),
+                                   (300, 200, 129), (600, 1500, 270)])
+def test_product_codes_past_k(m, n, k, rng):
+    """They have no effect up to the largest values that the type has under a scale."""
+    for kind, byte in (("bf16", 252), ("f16", 127 + 13)):
+        w = Weights(rng, n, k, byte, byte)
+        some = w.codes & 0xB                                # 1.5 at most
+        some[:, k:] = rng.choice([6, 7, 14, 15], some[:, k:].shape)
+        w.on[0].copy_(torch.from_numpy(O.pack(some)))
+        x = activations(rng, m, k, kind, True)[1]
+        x.mul_(2.0 ** -10)                                  # sums stay in fp32's range
+        want = x.view(m, k).double().cpu().numpy() @ O.values(some, w.scales, k).T
+        got = call_product(m, n, k, x, w, kind, "f32")
+        assert np.array_equal(got, rounded(want, "f32")), (kind, k)
+
+
+@pytest.mark.parametrize("m,n,ld_x,ld_w,ld_y", [
+    (3, 300, 1 << 30, 1 << 24, 1 << 30), (40, 300, 1 << 27, 1 << 24, 1 << 27),
+    (1100, 40000, 1 << 22, 1 << 17, 1 << 22), (300, 40000, 1 << 24, 1 << 17, 1 << 24)])
+def test_product_rows_far_apart(m, n, ld_x, ld_w, ld_y, rng):
+    """Offsets past 32 bits, in x, in the codes and in y."""
+    k = 264
+    x = torch.empty(m, ld_x, dtype=torch.bfloat16, device=DEV)
+    h = rng.integers(-8, 9, (m, k)).astype(np.float64)
+    x[:, :k] = torch.from_numpy(h).to(x)
+    w = Weights(rng, n, k, 126, 129)
+    codes = torch.empty(n, ld_w, dtype=torch.uint8, device=DEV)
+    codes[:, :144] = w.on[0]
+    y = torch.empty(m, ld_y, dtype=torch.bfloat16, device=DEV)
+    y[:, n] = -3
+    P.ifq_f4_matmul(P.f4_matmul_desc(m, n, k, P.IFQ_TYPE_BF16, None, ld_x, ld_w, ld_y), x, codes,
+                    w.on[1], y)
+    assert np.array_equal(y[:, :n].double().cpu().numpy(), rounded(h @ w.values.T, "bf16"))
+    assert (y[:, n] == -3).all()
 
 
 def test_product_infinities(rng):

@@ -192,6 +192,20 @@ def test_logprobs_strides(kind, rows, n, rng):
         view[:] = np.nan
 
 
+@pytest.mark.parametrize("rows,n,top", [(600, 5000, 0), (600, 5000, 7), (9, 50001, 0),
+                                        (9, 50001, 7), (600, 50001, 7)])
+def test_logprobs_rows_far_apart(rows, n, top, rng):
+    """Offsets past 32 bits."""
+    ld = -(-(5 << 30) // rows)
+    x = torch.empty(rows, ld, dtype=torch.bfloat16, device=DEV)
+    dense = torch.randn(rows, n, device=DEV).to(torch.bfloat16)
+    x[:, :n] = dense
+    tokens = torch.from_numpy(rng.integers(0, n, rows)).to(torch.int32).to(DEV)
+    want = call(dense, tokens, top, 1.0)
+    got = call(x, tokens, top, 1.0, ld_x=ld, kind=P.IFQ_TYPE_BF16, rows=rows, n=n)
+    assert all(b is None or np.array_equal(a, b) for a, b in zip(got, want))
+
+
 def test_logprobs_same_bits_on_a_shared_workspace(rng):
     """One workspace for calls of several sizes, as one program keeps it; parts in any order."""
     sizes = [(1, 128000, 20), (7, 33000, 64), (3, 50001, 0)]
