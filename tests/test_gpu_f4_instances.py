@@ -37,8 +37,10 @@ PRODUCTS = [
     (36, 41, 309, "f4_matmul_few<48, 2, 1, 2, 1>"),
     (68, 4108, 328, "f4_matmul_few<48, 2, 2, 3, 1>"),
     (33, 8235, 303, "f4_matmul_few<48, 2, 2, 3, 1>"),
-    (66, 8515, 448, "f4_matmul_few<48, 2, 4, 3, 1>"),
-    (37, 16526, 387, "f4_matmul_few<48, 2, 4, 3, 1>"),
+    (68, 8642, 304, "f4_matmul_few<48, 2, 3, 3, 1>"),
+    (70, 8514, 301, "f4_matmul_few<48, 2, 3, 3, 1>"),
+    (109, 8647, 392, "f4_matmul_few<48, 2, 4, 3, 1>"),
+    (101, 8744, 398, "f4_matmul_few<48, 2, 4, 3, 1>"),
     (50, 42, 352, "f4_matmul_few<64, 2, 1, 2, 1>"),
     (50, 43, 301, "f4_matmul_few<64, 2, 1, 2, 1>"),
     (56, 8434, 312, "f4_matmul_few<64, 2, 2, 3, 1>"),
@@ -73,8 +75,10 @@ GATED = [
     (33, 42, 338, "f4_matmul_few<48, 2, 1, 2, 2>"),
     (67, 2249, 312, "f4_matmul_few<48, 2, 2, 3, 2>"),
     (71, 2102, 330, "f4_matmul_few<48, 2, 2, 3, 2>"),
-    (33, 8308, 408, "f4_matmul_few<48, 2, 4, 3, 2>"),
-    (65, 4620, 397, "f4_matmul_few<48, 2, 4, 3, 2>"),
+    (72, 4162, 304, "f4_matmul_few<48, 2, 3, 3, 2>"),
+    (68, 4408, 307, "f4_matmul_few<48, 2, 3, 3, 2>"),
+    (104, 4121, 424, "f4_matmul_few<48, 2, 4, 3, 2>"),
+    (65, 6290, 421, "f4_matmul_few<48, 2, 4, 3, 2>"),
     (52, 41, 368, "f4_matmul_few<64, 2, 1, 2, 2>"),
     (50, 42, 333, "f4_matmul_few<64, 2, 1, 2, 2>"),
     (50, 4201, 376, "f4_matmul_few<64, 2, 2, 3, 2>"),
