@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ifq_serve.h"
 
@@ -309,7 +310,8 @@ __device__ __forceinline__ void rank(const uint64_t* list, int count, int k, uin
 // more maxima reach it, it is the k-th largest); of those equal to it a wave needs the
 // k first ones only.
 template <typename T, int PER, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 8 : 4) void logprobs_top(LogprobArgs a) {
+__global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(LogprobArgs a) {
+  typedef std::conditional_t<PER == 64, uint64_t, uint32_t> Bits;     // a lane's values
   constexpr int LANES = WAVES / 4;               // of a group
   constexpr int ABOVE = (64 + kMore) * LANES * PER;
   constexpr int LIST = std::max(ABOVE + 64 * WAVES, 64 * kMostParts);
@@ -336,13 +338,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 8 : 4) void logprobs_top(
   __syncthreads();
   {
     const float bar = value_of(bar_of(maxima, k, lane));
-    uint32_t above = 0, equal = 0;
+    Bits above = 0, equal = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      above |= v[i] > bar ? 1u << i : 0;
-      equal |= v[i] == bar ? 1u << i : 0;
+      above |= v[i] > bar ? (Bits)1 << i : 0;
+      equal |= v[i] == bar ? (Bits)1 << i : 0;
     }
-    int ties = __popc(equal);
+    int ties = __popcll(equal);
     ties += lane_xor<1>((uint32_t)ties);
     ties += lane_xor<2>((uint32_t)ties);
     ties += lane_xor<4>((uint32_t)ties);
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 8 : 4) void logprobs_top(
       constexpr int W = kRun<T>;
       int taken = 0;
       for (int i = 0; i < PER && taken < k; i += W) {
-        const uint32_t bits = equal >> i & ((1u << W) - 1);
+        const uint32_t bits = (uint32_t)(equal >> i) & ((1u << W) - 1);
         int before = taken, all = 0;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 8 : 4) void logprobs_top(
       }
     }
     while (const uint64_t some = __ballot(above != 0)) {
-      const int i = above ? __ffs(above) - 1 : 0;
+      const int i = above ? __ffsll((unsigned long long)above) - 1 : 0;
       float one = v[0];
 #pragma unroll
       for (int j = 1; j < PER; ++j) one = i == j ? v[j] : one;
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 8 : 4) void logprobs_top(
     t.all(a.c);
   }
   __syncthreads();
-  if (a.parts > 1) {
+  if (PER != 64 && a.parts > 1) {
     const int size = kPartFloats + 2 * k;
     float* all = a.part + (int64_t)(row - a.row0) * a.parts * size;
     if (wave == 0) {
@@ -468,20 +470,26 @@ constexpr int kPer = 32;
 // How a call is split: rows over launches, since there are 16384 counters of parts,
 // and each row over workgroups.
 struct Plan {
-  bool wide;                     // with top tokens: 16 waves of 32 values a lane, or 4 of 16
+  int32_t per;                   // with top tokens, values a lane: 16 waves of 64 or 32, or 4 of 16
   int32_t parts;
   int64_t rows;                  // of a launch
 };
 
 Plan plan_of(const ifq_logprobs_desc& d) {
-  Plan p = {false, 1, d.rows};
+  Plan p = {16, 1, d.rows};
   if (d.top) {
-    // us, narrow and wide (bfloat16, 10 top tokens): 1 x 16000 8.4 and 8.4, 256 x 16000 13.2
-    // and 11.3, 4000 x 16000 129 and 88, 1 x 50000 9.4 and 16.7, 64 x 50000 14.7 and 18.5,
-    // 64 x 128000 27 and 16, 1000 x 128000 269 and 113; but 1000 x 8000 22 and 26
+    // 4096 values a workgroup spread a row widely; 32768 and 65536 spare the join of parts or
+    // shorten it. us for 5 top tokens of bfloat16 rows, narrow and 64 values a lane: 16 x 33000
+    // 10.1 and 12.0, 96 x 33000 12.7 and 12.4, 40 x 65500 13.8 and 12.0; two parts of 32768 in the
+    // place of one of 65536: 256 x 33000 28 and 14, 1000 x 50001 98 and 58. Narrow and 32 values
+    // beyond 65536: 14 x 66000 11.3 and 11.9, 40 x 66000 14.1 and 12.1, 40 x 128000 19.2 and 13.2.
+    // There 64 values are slower again, with one workgroup on a CU and a join: 200 x 128000 32 and
+    // 40, 1000 x 100000 100 and 157. Up to 8192: 1000 x 8000 narrow 22, 32 values 26.
     const int64_t narrow = (d.n + 4095) / 4096;
-    p.wide = d.n > 8192 && (d.n <= 32768 || narrow * d.rows > 1536 || narrow > kMostParts);
-    p.parts = (int32_t)(p.wide ? (d.n + 32767) / 32768 : narrow);
+    if (d.n > 32768 && d.n <= 65536) p.per = narrow * d.rows > 640 ? 64 : 16;
+    else if (d.n > 8192 && (d.n <= 32768 || narrow * d.rows > 400 || narrow > kMostParts))
+      p.per = 32;
+    p.parts = (int32_t)(p.per == 16 ? narrow : (d.n + 1024 * p.per - 1) / (1024 * p.per));
   } else {
     // a few workgroups for each CU, and a turn for each wave at least
     const int64_t turns = (d.n + 64 * kPer - 1) / (64 * kPer);
@@ -504,7 +512,7 @@ size_t logprobs_workspace_bytes(const ifq_logprobs_desc& d) {
 
 int64_t logprobs_groups(const ifq_logprobs_desc& d) {
   const Plan p = plan_of(d);
-  return p.rows * p.parts * (p.wide ? 4 : 1);
+  return p.rows * p.parts * (p.per > 16 ? 4 : 1);
 }
 
 hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const int32_t* tokens,
@@ -535,7 +543,9 @@ hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const
       typedef decltype(zero) T;
       if (!d.top)
         hipLaunchKernelGGL((logprobs<T, kPer>), grid, dim3(64 * kWaves), 0, stream, a);
-      else if (p.wide)
+      else if (p.per == 64)
+        hipLaunchKernelGGL((logprobs_top<T, 64, 16>), grid, dim3(1024), 0, stream, a);
+      else if (p.per == 32)
         hipLaunchKernelGGL((logprobs_top<T, 32, 16>), grid, dim3(1024), 0, stream, a);
       else
         hipLaunchKernelGGL((logprobs_top<T, 16, 4>), grid, dim3(256), 0, stream, a);

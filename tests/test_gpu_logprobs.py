@@ -86,6 +86,38 @@ def test_logprobs_splits(kind, rows, n, top, rng):
     check(logits(rng, rows, n, kind), rng.integers(0, n, rows).tolist(), top)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,n,top", [
+    (71, 32769, 64), (80, 32769, 64), (50, 50001, 20), (49, 50001, 20), (41, 65535, 5),
+    (41, 65536, 64), (24, 65537, 33), (22, 65537, 33), (300, 40000, 3)])
+def test_logprobs_splits_of_batches(kind, rows, n, top, rng):
+    check(logits(rng, rows, n, kind), rng.integers(0, n, rows).tolist(), top)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("n,top", [(50001, 64), (65536, 7), (70000, 40)])
+def test_logprobs_hard_rows_of_batches(kind, n, top, rng):
+    """Ties, best tokens in one place, masks and rows without a distribution, in batches that
+    are split less."""
+    x = logits(rng, 66, n, kind, 0.01)
+    low = torch.finfo(x.dtype).min
+    for i in range(0, 66, 11):
+        x[i, n // 2:n // 2 + 100] += 50
+        x[i + 1, -200:] = -torch.arange(200, device=DEV).to(x.dtype) + 256
+        x[i + 2, ::3] = 7.0
+        x[i + 3] = -torch.inf
+        x[i + 3, i + 5:i + 8] = 1.0
+        x[i + 4] = low
+        x[i + 4, n - 3:] = 2.0
+        x[i + 5] = -torch.inf
+        x[i + 6, n - 1] = torch.nan
+        x[i + 7, 40000 + i] = torch.inf
+        x[i + 8] = torch.arange(n, device=DEV) % 4 * 1.0
+        x[i + 9] = 0.0
+        x[i + 9, ::2] = -0.0
+    check(x, [(i * 777) % n if i % 5 else -1 for i in range(66)], top)
+
+
 @pytest.mark.parametrize("n,top", [(4000, 64), (30000, 64), (60000, 40), (100000, 3)])
 def test_logprobs_best_in_one_place(n, top, rng):
     """The top tokens all in a few lanes, or all equal and everywhere."""
