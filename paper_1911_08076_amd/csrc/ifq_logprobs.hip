@@ -287,21 +287,27 @@ __device__ __forceinline__ int places(int* count, uint64_t some, int lane) {
   return __builtin_amdgcn_readfirstlane(first) + (int)__popcll(some & ((1ull << lane) - 1));
 }
 
-// Each key of a list at its place among the first k; a list of fewer leaves zeros. The list
-// has kRankRun - 1 keys of 0 behind it.
-constexpr int kRankRun = 8;
+// Each key of a list at its place among the first k; a list of fewer leaves zeros. LANES lanes
+// count for a key, eight others at a time each (in workgroups of 4 waves 4: 4000 x 4000 top 20
+// 23.9 -> 22.5 us; of 16 one: four spilled registers, 2000 x 32000 55 -> 60). The list has kRankRun
+// keys of 0 behind it.
+constexpr int kRankRun = 32;
+template <int LANES>
 __device__ __forceinline__ void rank(const uint64_t* list, int count, int k, uint64_t* best) {
-  for (int i = threadIdx.x; i < count; i += blockDim.x) {
+  const int part = threadIdx.x % LANES;
+  for (int i = threadIdx.x / LANES; i < count; i += blockDim.x / LANES) {
     const uint64_t key = list[i];
     int place = 0;
-    for (int j = 0; j < count; j += kRankRun) {
-      uint64_t some[kRankRun];
+    for (int j = 0; j < count; j += 8 * LANES) {
+      uint64_t some[8];
 #pragma unroll
-      for (int q = 0; q < kRankRun; ++q) some[q] = list[j + q];
+      for (int q = 0; q < 8; ++q) some[q] = list[j + 8 * part + q];
 #pragma unroll
-      for (int q = 0; q < kRankRun; ++q) place += some[q] > key;
+      for (int q = 0; q < 8; ++q) place += some[q] > key;
     }
-    if (place < k) best[place] = key;
+    if (LANES >= 2) place += lane_xor<1>((uint32_t)place);
+    if (LANES >= 4) place += lane_xor<2>((uint32_t)place);
+    if (part == 0 && place < k) best[place] = key;
   }
 }
 
@@ -323,9 +329,12 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
   const int64_t row = a.row0 + blockIdx.x / a.parts;
   const int own = blockIdx.x % a.parts, k = a.top;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  const int base = (own * WAVES + wave) * (64 * PER);
+  // parts of about the same size, so that the last one too has more groups than top tokens: with
+  // fewer all its values are ranked (8 x 200000 top 33 310 us, 17 with this)
+  const int from = a.chunks * own / a.parts, to = a.chunks * (own + 1) / a.parts;
+  const int base = (from + wave) * (64 * PER);
   float v[PER];
-  load_turn<T, PER>(x, base, a.n, lane, v);
+  load_turn<T, PER>(x, base, min(a.n, to * (64 * PER)), lane, v);
   Sums t = sums_of<PER>(v, a.c);
   uint32_t most = order_of(t.m);
   if (LANES >= 2) most = max(most, lane_xor<1>(most));
@@ -390,7 +399,7 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
   __syncthreads();
   if (threadIdx.x < kRankRun) list[count + threadIdx.x] = 0;
   __syncthreads();
-  rank(list, count, k, best);
+  rank<WAVES == 4 ? 4 : 1>(list, count, k, best);
   if (wave == 0) {
     t = {-INFINITY, 0.0f, 0.0f};
     if (lane < WAVES) t = sums[lane];
@@ -451,7 +460,7 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
     __syncthreads();
     if (threadIdx.x < kRankRun) list[count + threadIdx.x] = 0;
     __syncthreads();
-    rank(list, count, k, best);
+    rank<WAVES == 4 ? 4 : 1>(list, count, k, best);
     __syncthreads();
   }
   if (wave != 0) return;
@@ -533,7 +542,8 @@ hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const
   a.n = (int32_t)d.n;
   a.top = d.top;
   a.parts = p.parts;
-  a.chunks = (int32_t)((d.n + 64 * kPer - 1) / (64 * kPer));
+  const int turn = 64 * (d.top ? p.per : kPer);
+  a.chunks = (int32_t)((d.n + turn - 1) / turn);
   a.scale = d.scale;
   a.c = d.scale * 1.4426950408889634f;
   for (int64_t row = 0; row < d.rows; row += p.rows) {

@@ -89,7 +89,8 @@ def test_logprobs_splits(kind, rows, n, top, rng):
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("rows,n,top", [
     (71, 32769, 64), (80, 32769, 64), (50, 50001, 20), (49, 50001, 20), (41, 65535, 5),
-    (41, 65536, 64), (24, 65537, 33), (22, 65537, 33), (300, 40000, 3)])
+    (41, 65536, 64), (24, 65537, 33), (22, 65537, 33), (300, 40000, 3),
+    (8, 200000, 33), (2, 5000, 64), (1, 1015809, 64)])
 def test_logprobs_splits_of_batches(kind, rows, n, top, rng):
     check(logits(rng, rows, n, kind), rng.integers(0, n, rows).tolist(), top)
 
