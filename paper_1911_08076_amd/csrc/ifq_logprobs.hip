@@ -210,7 +210,8 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, const 
 }
 
 // Without top tokens. One row or a part of it to a workgroup; its waves take turns of 64 *
-// PER values, which stay in registers between the search for the largest and the sums.
+// PER values, which stay in registers between the search for the largest and the sums. Bound
+// by memory: 4000 x 32000 float32 87 us, 5.9 TB/s.
 template <typename T, int PER>
 __global__ __launch_bounds__(64 * kWaves) void logprobs(LogprobArgs a) {
   __shared__ Sums sums[kWaves];
@@ -312,7 +313,8 @@ __device__ __forceinline__ void rank(const uint64_t* list, int count, int k, uin
 }
 
 // With top tokens. Every wave takes one turn, so that its values stay in registers until
-// the bar is known. Values above the bar are in k + kMore groups at most (where
+// the bar is known; a chain of load, maxima, bar, list and places, for a row's parts twice (1 x
+// 128000 top 20 10.7 us, 96 x 50001 top 5 without a join 13.1). Values above the bar are in k + kMore groups at most (where
 // more maxima reach it, it is the k-th largest); of those equal to it a wave needs the
 // k first ones only.
 template <typename T, int PER, int WAVES>
