@@ -15,7 +15,9 @@ namespace {
 //   log p(x) = scale * (x - M) - ln S,  entropy = ln S - ln 2 * E / S
 // Both terms of the entropy are positive, so nothing cancels. Parts of a row keep
 // sums for a maximum of their own; with d = c * (M_part - M) their share is
-// 2^d S and 2^d (E + d S).
+// 2^d S and 2^d (E + d S). Differences are taken in halves and times twice the factor: x - M
+// may leave fp32's range where scale * (x - M) does not. (x - M) / 2 is one operation,
+// fma(x, 1/2, -M/2), with the bits of x - M wherever that is in the range.
 //
 // The top tokens go by a key of 64 bits: the value, as an integer of the same
 // order, over the complement of the index, so that keys differ and equal values
@@ -36,7 +38,7 @@ struct LogprobArgs {
   int64_t row0;                  // first row of this launch
   int32_t n, top, parts;
   int32_t chunks;                // of a row, each a wave's turn
-  float scale, c;
+  float scale2, c2;              // twice scale and c
 };
 
 constexpr float kLn2 = 0.69314718055994531f;
@@ -83,26 +85,31 @@ __device__ __forceinline__ uint64_t key_of(float v, int index) {
 
 __device__ __forceinline__ int index_of(uint64_t key) { return (int)~(uint32_t)key; }
 
+// (v - from) / 2 for half = from / 2, without leaving fp32's range.
+__device__ __forceinline__ float half_from(float v, float half) {
+  return __builtin_fmaf(v, 0.5f, -half);
+}
+
 struct Sums {
   float m, s, e;
   // the sums as they go by a maximum that is as large at least
-  __device__ __forceinline__ void to(float top, float c) {
+  __device__ __forceinline__ void to(float top, float c2) {
     const float r = top == -INFINITY ? 0.0f : top;
     // an empty part has no share (and its maximum none either)
-    const float d = s == 0.0f ? 0.0f : c * (m - r), f = __builtin_amdgcn_exp2f(d);
+    const float d = s == 0.0f ? 0.0f : c2 * half_from(m, 0.5f * r), f = __builtin_amdgcn_exp2f(d);
     e = f == 0.0f ? 0.0f : f * (e + d * s);    // a share of 0 adds nothing, also where d is -infinity
     s *= f;
     m = top;
   }
-  __device__ __forceinline__ void add(Sums o, float c) {
+  __device__ __forceinline__ void add(Sums o, float c2) {
     const float top = fmaxf(m, o.m);
-    to(top, c);
-    o.to(top, c);
+    to(top, c2);
+    o.to(top, c2);
     s += o.s;
     e += o.e;
   }
   // over the lanes
-  __device__ __forceinline__ void all(float c) {
+  __device__ __forceinline__ void all(float c2) {
     float top = m;
     top = fmaxf(top, lane_xor<1>(top));
     top = fmaxf(top, lane_xor<2>(top));
@@ -110,7 +117,7 @@ struct Sums {
     top = fmaxf(top, lane_xor<8>(top));
     top = fmaxf(top, lane_xor<16>(top));
     top = fmaxf(top, lane_xor<32>(top));
-    to(top, c);
+    to(top, c2);
     s += lane_xor<1>(s), e += lane_xor<1>(e);
     s += lane_xor<2>(s), e += lane_xor<2>(e);
     s += lane_xor<4>(s), e += lane_xor<4>(e);
@@ -164,15 +171,15 @@ __device__ __forceinline__ void load_turn(const T* row, int base, int n, int lan
 
 // A turn's sums of a lane.
 template <int PER>
-__device__ __forceinline__ Sums sums_of(const float* v, float c) {
+__device__ __forceinline__ Sums sums_of(const float* v, float c2) {
   float m = v[0];
 #pragma unroll
   for (int i = 1; i < PER; ++i) m = fmaxf(m, v[i]);
   Sums u = {m, 0.0f, 0.0f};
-  const float r = m == -INFINITY ? 0.0f : m;
+  const float half = m == -INFINITY ? 0.0f : 0.5f * m;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const float z = c * (v[i] - r), e = __builtin_amdgcn_exp2f(z);
+    const float z = c2 * half_from(v[i], half), e = __builtin_amdgcn_exp2f(z);
     u.s += e;
     u.e = __builtin_fmaf(fmaxf(z, -1e4f), e, u.e);     // 0 where e is, z -infinity or not
   }
@@ -183,15 +190,15 @@ __device__ __forceinline__ Sums sums_of(const float* v, float c) {
 // 0); with a NaN or an infinity in it (S is NaN) it has no distribution.
 struct Row {
   bool none;
-  float from, log;
+  float half, log;               // of the largest logit; of the sum
   __device__ __forceinline__ explicit Row(const Sums& t) {
     const bool empty = t.s == 0.0f;
     none = t.s != t.s;
-    from = empty ? 0.0f : t.m;
+    half = empty ? 0.0f : 0.5f * t.m;
     log = empty ? 0.0f : logf(t.s);
   }
-  __device__ __forceinline__ float logprob(float v, float scale) const {
-    return scale * (v - from) - log;
+  __device__ __forceinline__ float logprob(float v, float scale2) const {
+    return scale2 * half_from(v, half) - log;
   }
 };
 
@@ -204,7 +211,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, const 
     const int token = a.tokens[row];
     float p = 0.0f;
     if (token >= a.n) p = bits_f32(0x7FC00000u);
-    else if (token >= 0) p = f.logprob((float)x[token], a.scale);
+    else if (token >= 0) p = f.logprob((float)x[token], a.scale2);
     a.logprob[row] = p;
   }
 }
@@ -226,14 +233,14 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs(LogprobArgs a) {
   for (int chunk = from + wave; chunk < to; chunk += kWaves) {
     float v[PER];
     load_turn<T, PER>(x, chunk * (64 * PER), a.n, lane, v);
-    t.add(sums_of<PER>(v, a.c), a.c);
+    t.add(sums_of<PER>(v, a.c2), a.c2);
   }
-  t.all(a.c);
+  t.all(a.c2);
   if (lane == 0) sums[wave] = t;
   __syncthreads();
   if (wave == 0) {
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) t.add(sums[w], a.c);
+    for (int w = 1; w < kWaves; ++w) t.add(sums[w], a.c2);
   }
   if (a.parts > 1) {
     float* all = a.part + (int64_t)(row - a.row0) * a.parts * kPartFloats;
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs(LogprobArgs a) {
       const f32x2 ms = get_pair(all + lane * kPartFloats), e = get_pair(all + lane * kPartFloats + 2);
       t = {ms[0], ms[1], e[0]};
     }
-    t.all(a.c);
+    t.all(a.c2);
   }
   if (threadIdx.x == 0) finish(a, row, x, t);
 }
@@ -337,14 +344,14 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
   const int base = (from + wave) * (64 * PER);
   float v[PER];
   load_turn<T, PER>(x, base, min(a.n, to * (64 * PER)), lane, v);
-  Sums t = sums_of<PER>(v, a.c);
+  Sums t = sums_of<PER>(v, a.c2);
   uint32_t most = order_of(t.m);
   if (LANES >= 2) most = max(most, lane_xor<1>(most));
   if (LANES >= 4) most = max(most, lane_xor<2>(most));
   if (lane % LANES == 0) maxima[threadIdx.x / LANES] = most;
   if (threadIdx.x < 64) best[threadIdx.x] = 0;
   if (threadIdx.x == 0) count = 0;
-  t.all(a.c);
+  t.all(a.c2);
   if (lane == 0) sums[wave] = t;
   __syncthreads();
   {
@@ -405,7 +412,7 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
   if (wave == 0) {
     t = {-INFINITY, 0.0f, 0.0f};
     if (lane < WAVES) t = sums[lane];
-    t.all(a.c);
+    t.all(a.c2);
   }
   __syncthreads();
   if (PER != 64 && a.parts > 1) {
@@ -447,7 +454,7 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
         const f32x2 e = get_pair(all + (int64_t)lane * size + 2);
         t = {ms[0], ms[1], e[0]};
       }
-      t.all(a.c);
+      t.all(a.c2);
     }
     __syncthreads();
     const uint32_t bar = bar_of(maxima, k, lane);
@@ -471,7 +478,7 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
     const Row f(t);
     const uint64_t key = best[lane];
     a.top_logprobs[row * a.ld_top + lane] =
-        f.none ? bits_f32(0x7FC00000u) : f.logprob(value_of((uint32_t)(key >> 32)), a.scale);
+        f.none ? bits_f32(0x7FC00000u) : f.logprob(value_of((uint32_t)(key >> 32)), a.scale2);
     a.top_tokens[row * a.ld_top + lane] = f.none ? -1 : index_of(key);
   }
 }
@@ -546,8 +553,8 @@ hipError_t launch_logprobs(const ifq_logprobs_desc& d, const void* logits, const
   a.parts = p.parts;
   const int turn = 64 * (d.top ? p.per : kPer);
   a.chunks = (int32_t)((d.n + turn - 1) / turn);
-  a.scale = d.scale;
-  a.c = d.scale * 1.4426950408889634f;
+  a.scale2 = 2.0f * d.scale;
+  a.c2 = a.scale2 * 1.4426950408889634f;
   for (int64_t row = 0; row < d.rows; row += p.rows) {
     a.row0 = row;
     const dim3 grid((uint32_t)(std::min(p.rows, d.rows - row) * p.parts));

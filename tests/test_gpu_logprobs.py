@@ -207,6 +207,46 @@ def test_logprobs_temperatures(scale, rng):
     check(logits(rng, 1, 50000, "bf16"), [7], 5, scale=scale)
 
 
+def over_the_range(rng, n, kind):
+    """Rows whose values differ by more than fp32's largest number."""
+    most = torch.finfo(TYPES[kind][0]).max
+    x = torch.from_numpy(rng.uniform(-most, most, (5, n)).astype(np.float32)).to(DEV)
+    x[1] = -most
+    x[1, n // 2] = most
+    x[2] = -most
+    x[2, n - 1] = most                       # parts whose maxima are as far apart
+    x[3, :n - 1:2] = -torch.inf
+    x[4] = -most
+    x[4, 0] = most
+    x[4, 1:n - 1] = -torch.inf
+    return x.to(TYPES[kind][0]), [0, n - 1, 0, n - 1, n - 1]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("n,top", [(2, 2), (90, 0), (90, 20), (5000, 0), (5000, 64), (40000, 5),
+                                   (70000, 0), (70000, 5)])
+def test_logprobs_differences_past_the_range(n, top, kind, rng):
+    """What the scale brings back into it counts."""
+    for scale in (1e-37, 1e-30, 0.25, 0.5, 1.0):
+        check(*over_the_range(rng, n, kind), top, scale=scale)
+
+
+@pytest.mark.parametrize("n,top", [(90, 20), (5000, 0), (70000, 5)])
+def test_logprobs_scales_below_the_normal_range(n, top, rng):
+    """The scale in units of log2 e is then off by 2^-150 at most, a difference's half (below
+    2^128) times it by 2^-22, a term's logarithm with it; |z| is below 2 in these rows, so that a
+    mean of z under weights off by 2^-22 each way is off by 2 * 2 * 2^-22 and by 2^-22 of its own."""
+    x, tokens = over_the_range(rng, n, "f32")
+    scale = 2.0 ** -128
+    got = call(x, torch.tensor(tokens, dtype=torch.int32, device=DEV), top, scale)
+    (lp, h, best, at), (blp, bh, bbest) = O.logprobs(x.double().cpu().numpy(), tokens, top, scale)
+    within(got[0], lp, blp + 2.0 ** -22)
+    within(got[1], h, bh + 6 * 2.0 ** -22)
+    if top:
+        assert np.array_equal(got[3], at)
+        within(got[2], best, bbest + 2.0 ** -22)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,n", [(4, 601), (2, 30001)])
 def test_logprobs_strides(kind, rows, n, rng):
