@@ -199,11 +199,28 @@ __device__ __forceinline__ typename Half<T>::x8 operand(uint32_t w, float s) {
 }
 
 // The activation in fp32. Each form keeps its relative precision where it is small.
-__device__ __forceinline__ float activate(float g, int kind) {
-  if (kind == IFQ_ACT_SILU) return g / (1.0f + expf(-g));
-  if (kind == IFQ_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678118654752f);
-  // g/2 (1 + tanh(u)) = g / (1 + e^-2u), u = sqrt(2/pi) (g + 0.044715 g^3)
-  return g / (1.0f + expf(g * (g * g * 0.044715f + 1.0f) * -1.5957691216057308f));
+__device__ __forceinline__ f32x4 activate(f32x4 g, int kind) {
+  f32x4 a, q;
+  if (kind == IFQ_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = 0.5f * g[i] * erfcf(g[i] * -0.70710678118654752f);
+    return q;
+  }
+  // g / (1 + e^a); g/2 (1 + tanh(u)) with a = -2u, u = sqrt(2/pi) (g + 0.044715 g^3)
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    a[i] = kind == IFQ_ACT_SILU ? -g[i]
+                                : g[i] * (g[i] * g[i] * 0.044715f + 1.0f) * -1.5957691216057308f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = g[i] / (1.0f + expf(a[i]));
+  // Beyond 88.7 e^a leaves fp32's range while the quotient is still in it: there the 1 does not
+  // count, and it is g e^-64 e^(64 - a). Behind a branch, since few waves have such lanes
+  if (__ballot(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) > 88.0f) != 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (a[i] > 88.0f) q[i] = g[i] * 1.6038108905486378e-28f * expf(64.0f - a[i]);
+  }
+  return q;
 }
 
 // Four sums of a row of y, or what is left of it; a row may begin at any element.
@@ -458,9 +475,7 @@ __global__ __launch_bounds__(XR <= 16 ? 1024 : 512) void f4_matmul_few(F4MatmulA
       v[z] = *p;
       for (int w = 1; w < groups; ++w) v[z] += p[w * WN * NT * MT * 64];
     }
-    if constexpr (HALVES == 2)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[0][e] = activate(v[0][e], a.activation) * v[1][e];
+    if constexpr (HALVES == 2) v[0] = activate(v[0], a.activation) * v[1];
     store4(a.y, a.y_type, m * a.ld_y + n, v[0], a.n - n);
   }
 }
@@ -658,12 +673,11 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs 
       for (int e = 0; e < 4; ++e) {
         const int n = n0 + 32 * (z / HALVES) + 8 * e + 4 * h;
         if (n >= a.n) continue;
-        f32x4 v;
+        f32x4 v, u;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v[q] = acc[x][z][4 * e + q];
-          if (HALVES == 2) v[q] = activate(v[q], a.activation) * acc[x][z + HALVES - 1][4 * e + q];
-        }
+        for (int q = 0; q < 4; ++q)
+          v[q] = acc[x][z][4 * e + q], u[q] = acc[x][z + HALVES - 1][4 * e + q];
+        if constexpr (HALVES == 2) v = activate(v, a.activation) * u;
         store4(a.y, a.y_type, m * a.ld_y + n, v, a.n - n);
       }
   }

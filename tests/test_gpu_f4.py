@@ -332,6 +332,35 @@ def test_gated(m, n, k, kind, y_kind, act, rng):
     check_gated(rng, m, n, k, kind, y_kind, act)
 
 
+@pytest.mark.parametrize("m,n", [(7, 40), (300, 50), (4000, 3000)])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_gated_activations_far_below_zero(act, m, n):
+    """Down to where fp32 ends, beside sums that bring them back: a sum is one activation times
+    1, so g and u are exact. Relative as in gated_bound; what an activation below fp32's normal
+    range loses is 2^-149 times 16 at most (a rounding of erfc times |g|/2 below 8, two more),
+    times u."""
+    lo, hi = {"silu": (60, 103), "gelu": (12, 14), "gelu_tanh": (9, 10.7)}[act]
+    g = -torch.linspace(lo, hi, m, dtype=torch.float64).to(torch.bfloat16)
+    u = (2.0 ** 100) * (1 + torch.arange(m) % 2).to(torch.bfloat16)
+    x = torch.zeros(m, 32, dtype=torch.bfloat16)
+    x[:, 0], x[:, 1] = g, u
+    codes = torch.zeros(2, n, 16, dtype=torch.uint8)
+    codes[0, :, 0], codes[1, :, 0] = 0x02, 0x20             # 1 in column 0, in column 1
+    scales = torch.full((1, n, 4), 127, dtype=torch.uint8, device=DEV)
+    y = torch.empty(m, n, device=DEV)
+    codes = codes.to(DEV)
+    P.ifq_f4_gated(P.f4_matmul_desc(m, n, 32, P.IFQ_TYPE_BF16, P.IFQ_TYPE_F32,
+                                    activation=ACTS[act]), x.to(DEV), codes[0], scales, codes[1],
+                   scales, y)
+    g, u = g.double().numpy()[:, None], u.double().numpy()[:, None]
+    want = O.activate(g, ACTS[act]) * u
+    size = {"silu": np.abs(g), "gelu": g * g + 1,
+            "gelu_tanh": 1.5957691 * np.abs(g + 0.044715 * g ** 3)}[act]
+    bound = np.abs(want) * (4 * size + 16) * 2.0 ** -23 + 16 * 2.0 ** -149 * u
+    off = np.abs(y.double().cpu().numpy() - want)
+    assert (off <= bound).all(), (off / bound).max()
+
+
 @pytest.mark.parametrize("m", [1, 7, 40, 150, 300])
 def test_gated_strides(m, rng):
     check_gated(rng, m, 77, 272, "bf16", "f32", "silu", ld_x=275, ld_w=160, ld_y=81)
