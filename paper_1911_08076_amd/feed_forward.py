@@ -61,6 +61,8 @@ class F4Weight:
 
     def values(self, dtype=torch.float32):
         """What they stand for, [out][in]."""
+        if dtype not in _TYPES:
+            raise ValueError("values of %s" % dtype)
         out = torch.empty(self.n, self.k, dtype=dtype, device=self.codes.device)
         with _on(self.codes.device):
             P.ifq_f4_dequantize(P.f4_weights_desc(self.n, self.k, _TYPES[dtype]), self.codes,

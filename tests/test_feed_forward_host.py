@@ -68,6 +68,16 @@ def test_weights_that_do_not_fit_are_refused(launches):
     assert launches.seen == []
 
 
+def test_values_of_a_type_that_is_not_known_are_refused(launches):
+    weight = F.F4Weight(empty(96, 64))
+    launches.seen.clear()
+    for dtype in (torch.float64, torch.int32):
+        with pytest.raises(ValueError):
+            weight.values(dtype)
+    assert launches.seen == []
+    assert weight.values(F32).dtype == F32 and weight.values(BF16).shape == (96, 64)
+
+
 @pytest.mark.parametrize("x", [
     lambda: empty(3, 64, dev="cpu"), lambda: empty(3, 64, dev="cuda:1"), lambda: empty(3, 63),
     lambda: empty(3, 64, dtype=F32), lambda: empty(64, 3).t(), lambda: empty(64)])
