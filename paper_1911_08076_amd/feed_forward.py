@@ -46,7 +46,7 @@ class F4Weight:
     """Weights [out][in] as codes and scales (ifq_f4_quantize)."""
 
     def __init__(self, weight):
-        _check_rows(weight, weight.shape[-1], tuple(_TYPES), weight.device)
+        _check_rows(weight, weight.shape[-1:].numel(), tuple(_TYPES), weight.device)
         dev = weight.device
         if dev.type != "cuda":
             raise ValueError("weights on a GPU expected, got them on %s" % dev)
@@ -140,7 +140,7 @@ def token_logprobs(logits, tokens=None, top=0, scale=1.0, workspace=None):
     softmax(scale * logits), the entropy, and the `top` most probable tokens, of logits
     [rows][vocabulary] in bfloat16, float16 or float32 (ifq_logprobs)."""
     dev = logits.device
-    _check_rows(logits, logits.shape[-1], tuple(_TYPES), dev)
+    _check_rows(logits, logits.shape[-1:].numel(), tuple(_TYPES), dev)
     if dev.type != "cuda":
         raise ValueError("logits on a GPU expected, got them on %s" % dev)
     rows, n = logits.shape

@@ -68,6 +68,14 @@ def test_weights_that_do_not_fit_are_refused(launches):
     assert launches.seen == []
 
 
+def test_tensors_without_dimensions_are_refused(launches):
+    with pytest.raises(ValueError):
+        F.F4Weight(empty())
+    with pytest.raises(ValueError):
+        F.token_logprobs(empty())
+    assert launches.seen == []
+
+
 def test_values_of_a_type_that_is_not_known_are_refused(launches):
     weight = F.F4Weight(empty(96, 64))
     launches.seen.clear()
