@@ -70,9 +70,9 @@ def test_weights_that_do_not_fit_are_refused(launches):
 
 def test_tensors_without_dimensions_are_refused(launches):
     with pytest.raises(ValueError):
-        F.F4Weight(empty())
+        F.F4Weight(empty(1)[0])
     with pytest.raises(ValueError):
-        F.token_logprobs(empty())
+        F.token_logprobs(empty(1)[0])
     assert launches.seen == []
 
 
