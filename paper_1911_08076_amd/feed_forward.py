@@ -42,6 +42,13 @@ def _overlap(a, b):
             b.data_ptr() < a.data_ptr() + a.numel() * a.element_size())
 
 
+def _check_tokens(tokens, rows, device):
+    if tokens is not None and (tokens.shape != (rows,) or tokens.dtype != torch.int32 or
+                               not tokens.is_contiguous() or tokens.device != device):
+        raise ValueError("tokens: dense int32 of shape (%d,) on %s expected, got %s of %s on %s" % (
+            rows, device, tuple(tokens.shape), tokens.dtype, tokens.device))
+
+
 class F4Weight:
     """Weights [out][in] as codes and scales (ifq_f4_quantize)."""
 
@@ -144,10 +151,7 @@ def token_logprobs(logits, tokens=None, top=0, scale=1.0, workspace=None):
     if dev.type != "cuda":
         raise ValueError("logits on a GPU expected, got them on %s" % dev)
     rows, n = logits.shape
-    if tokens is not None and (tokens.shape != (rows,) or tokens.dtype != torch.int32 or
-                               not tokens.is_contiguous() or tokens.device != dev):
-        raise ValueError("tokens: dense int32 of shape (%d,) on %s expected, got %s of %s on %s" % (
-            rows, dev, tuple(tokens.shape), tokens.dtype, tokens.device))
+    _check_tokens(tokens, rows, dev)
     d = P.logprobs_desc(rows, n, _TYPES[logits.dtype], top, scale)
     with _on(dev):
         logprob = None if tokens is None else torch.empty(rows, device=dev)
@@ -170,5 +174,8 @@ class Classifier:
 
     def __call__(self, x, tokens=None, top=1, scale=1.0):
         """x [m][hidden] -> TokenLogprobs of its rows (token_logprobs)."""
+        weight = self.linear.weight
+        _check_rows(x, weight.k, _HALVES, weight.codes.device)
+        _check_tokens(tokens, x.shape[0], x.device)
         logits = self.linear(x, dtype=torch.float32)
         return token_logprobs(logits, tokens, top, scale, self.workspace)

@@ -143,6 +143,18 @@ def test_logits_and_tokens_that_do_not_fit_are_refused(launches):
     assert launches.seen == []
 
 
+def test_a_classifier_refuses_tokens_before_its_product(launches):
+    classifier = F.Classifier(empty(50, 64))
+    launches.seen.clear()
+    for t in (empty(3, dtype=torch.int64), empty(4, dtype=torch.int32), empty(3, 1, dtype=torch.int32),
+              empty(3, dtype=torch.int32, dev="cuda:1"), empty(6, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            classifier(empty(3, 64), t)
+    assert launches.seen == []
+    classifier(empty(3, 64), empty(3, dtype=torch.int32))
+    assert [name for name, _ in launches.seen] == ["ifq_f4_matmul", "ifq_logprobs"]
+
+
 @pytest.mark.parametrize("dev", ["cuda:0", "cuda:1"])
 def test_launches_go_to_the_layers_gpu(launches, dev):
     feed = F.FeedForward(empty(96, 64, dev=dev), empty(96, 64, dev=dev), empty(64, 96, dev=dev),
