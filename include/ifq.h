@@ -930,9 +930,9 @@ IFQ_API ifq_status ifq_f4_quantize(const ifq_f4_weights_desc* d, const void* x, 
 
 /*
  * The values that codes and scales stand for, rounded to x's type: exact in
- * bfloat16 and float32, whose overflow (codes of 4 and more under 2^126 and 2^127) is
- * infinite, and in float16 from 2^-24 to 65504. Codes that end in columns past k and
- * scales of groups past k may be anything.
+ * bfloat16 and float32, whose overflow (magnitudes of 4 and more under 2^126, of 2 and more
+ * under 2^127) is infinite, and in float16 from 2^-24 to 65504 (from 65536 on infinite). Codes
+ * that end in columns past k and scales of groups past k may be anything.
  */
 IFQ_API ifq_status ifq_f4_dequantize(const ifq_f4_weights_desc* d, const void* codes,
                                      const void* scales, void* x, hipStream_t stream);
@@ -978,8 +978,8 @@ IFQ_API const char* ifq_f4_gated_kernel_name(const ifq_f4_matmul_desc* d);
  *   y[i][j] = sum over k of x[i][k] * w[j][k]
  * with w the values that codes and scales stand for in x's type (float16: rounded
  * where they are below 2^-24 or above 65504), sums in fp32, rounded once to y's type.
- * Codes of columns past k may be any that are finite in x's type (the quantizer's are 0),
- * scales of groups past k anything.
+ * Codes of columns past k may be any that are finite in x's type under their group's scale
+ * (ifq_f4_dequantize says which; the quantizer's are 0), scales of groups past k anything.
  *   x          device [m][ld_x], aligned to its element
  *   w          device codes [n][ld_w], 16-byte aligned
  *   w_scales   device uint8 [ceil(k/128)][n][4], 4-byte aligned

@@ -255,6 +255,21 @@ def test_product_codes_past_k(m, n, k, rng):
         assert np.array_equal(got, rounded(want, "f32")), (kind, k)
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 70, 1), (20, 100, 287), (600, 1500, 270)])
+def test_product_codes_past_k_under_the_largest_scales(m, n, k, rng):
+    """3 under 2^126 and 1.5 under 2^127 are the largest that bfloat16 has there."""
+    for byte, far in ((253, [5, 13]), (254, [3, 11])):
+        w = Weights(rng, n, k, byte, byte)
+        some = w.codes & 9                                  # 0.5 at most
+        some[:, k:] = rng.choice(far, some[:, k:].shape)
+        w.on[0].copy_(torch.from_numpy(O.pack(some)))
+        x = activations(rng, m, k, "bf16", True)[1]
+        x.mul_(2.0 ** -13)                                  # 300 times 8 times 2^126 times this
+        want = x.view(m, k).double().cpu().numpy() @ O.values(some, w.scales, k).T
+        got = call_product(m, n, k, x, w, "bf16", "f32")
+        assert np.array_equal(got, rounded(want, "f32")), byte
+
+
 @pytest.mark.parametrize("m,n,ld_x,ld_w,ld_y", [
     (3, 300, 1 << 30, 1 << 24, 1 << 30), (40, 300, 1 << 27, 1 << 24, 1 << 27),
     (1100, 40000, 1 << 22, 1 << 17, 1 << 22), (300, 40000, 1 << 24, 1 << 17, 1 << 24)])

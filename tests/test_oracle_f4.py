@@ -19,6 +19,19 @@ def test_code_values():
         assert O.VALUES[c] == (-v if c & 8 else v)
 
 
+def test_codes_that_overflow():
+    """bfloat16 and float32: 4 and more under 2^126, 2 and more under 2^127; float16: from 65536."""
+    codes = np.tile(np.arange(16, dtype=np.uint8), (255, 2))
+    scales = np.full((1, 255, 4), 255, np.uint8)
+    scales[0, :, 0] = np.arange(255)
+    held = torch.from_numpy(O.values(codes, scales, 16))
+    magnitude, e = torch.from_numpy(np.tile(O.MAGNITUDES, 2)), torch.arange(255)[:, None] - 127
+    for dtype in (torch.float32, torch.bfloat16):
+        assert torch.equal(held.to(dtype).isinf(), (magnitude >= 4) & (e == 126) |
+                           (magnitude >= 2) & (e == 127))
+    assert torch.equal(held.half().isinf(), held.abs() >= 65536)
+
+
 def test_codes_are_the_nearest(rng):
     v = np.concatenate([rng.uniform(-7, 7, 2000), (O.MAGNITUDES[:-1] + O.MAGNITUDES[1:]) / 2,
                         O.MAGNITUDES, [-0.0, 6.9, -7.0]])
