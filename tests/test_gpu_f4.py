@@ -239,6 +239,23 @@ def test_product_values_at_the_ends_of_the_range(m, n, rng):
             assert np.array_equal(got, rounded(h @ held.T, "f32")), (kind, byte)
 
 
+@pytest.mark.parametrize("m,n", [(3, 70), (70, 100), (600, 1500), (4000, 3000)])
+def test_product_values_below_the_normal_range(m, n, rng):
+    """Activations, weights and outputs there, of each type. Whole numbers up to 8 times codes of
+    halves: sums are whole numbers of half the product of both units, below 2^14 of them in 96
+    columns, and exact in fp32 from 2^-149 on."""
+    k = 96
+    for kind, unit, scale in (("bf16", -133, 100), ("bf16", -133, 8), ("f16", -24, 10),
+                              ("f16", -24, 0), ("bf16", -6, -126), ("bf16", 0, -127), ("f16", 0, -23)):
+        w = Weights(rng, n, k, 127 + scale, 127 + scale)
+        x = activations(rng, m, k, kind, True)[1]
+        x.mul_(2.0 ** unit)
+        want = x.view(m, k).double().cpu().numpy() @ w.values.T
+        for y_kind in ("f32", "bf16", "f16"):
+            got = call_product(m, n, k, x, w, kind, y_kind)
+            assert np.array_equal(got, rounded(want, y_kind)), (kind, unit, scale, y_kind)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 70, 1), (3, 70, 100), (20, 100, 287), (70, 100, 33),
                                    (300, 200, 129), (600, 1500, 270)])
 def test_product_codes_past_k(m, n, k, rng):
