@@ -201,6 +201,30 @@ def test_logprobs_orders(n, rng):
             check(x.to(TYPES[kind][0]), [n - 1] * 8, top)
 
 
+@pytest.mark.parametrize("kind,unit", [("bf16", 2.0 ** -133), ("f16", 2.0 ** -24),
+                                       ("f32", 2.0 ** -149)])
+@pytest.mark.parametrize("n,top", [(100, 20), (3000, 64), (50000, 5)])
+def test_logprobs_values_below_the_normal_range(n, top, kind, unit, rng):
+    """They are ordered as others are."""
+    x = torch.from_numpy(rng.integers(-30, 31, (4, n)) * unit).to(TYPES[kind][0]).to(DEV)
+    x[1].abs_().neg_()
+    x[2] = torch.arange(n, device=DEV) % 40 * unit
+    check(x, [0, 1, 2, n - 1], top)
+    check(x, [0, 1, 2, n - 1], top, scale=2.0 ** 64)
+
+
+@pytest.mark.parametrize("n,top", [(33000, 33), (50001, 20), (100000, 64), (131072, 40)])
+def test_logprobs_one_range_of_tokens(n, top, rng):
+    """All else is masked, so that fewer groups of values than top tokens hold any."""
+    for kind, value in (("bf16", -np.inf), ("f32", torch.finfo(torch.float32).min)):
+        x = logits(rng, 6, n, kind)
+        for i, (first, last) in enumerate(((0, 4096), (2000, 6096), (n - 3000, n), (16000, 16010),
+                                           (n // 2, n // 2 + 1024), (n // 3, n // 3 + 5000))):
+            x[i, :first] = value
+            x[i, last:] = value
+        check(x, [0, 2000, n - 1, 16005, n // 2, n // 3], top)
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-3, 100.0, 2.0 ** 64])
 def test_logprobs_temperatures(scale, rng):
     check(logits(rng, 4, 3000, "f32"), [1, 2, 3, 4], 5, scale=scale)
