@@ -320,11 +320,16 @@ __device__ __forceinline__ int turned(int q) { return (q & 1) << 1 ^ (q >> 1 & 1
 // of one group and 4-11 of the next, and these then spread over all 64 banks.
 //
 // DIRECT: x goes from memory into LDS; it needs 16-byte aligned rows of whole cells.
-// Otherwise it goes through registers, a block ahead.
+// Otherwise it goes through registers, and every block waits for all loads on their way: its
+// own cells, those of the next block, just asked for, and the weights of every stage. Only other
+// workgroups hide that. us with k of 4096 and of 4095: 7 x 4096 5.4 and 5.9, 24 x 4096 7.4 and
+// 13.2, 41 x 4096 10.0 and 21.0, gated 7 x 9001 13.5 and 19.3, gated 41 x 9001 19.8 and 28.0.
 //
-// Up to some 16 rows bound by memory: 1 x 4096 x 14336 8.0 us (3.9 TB/s with the launch), 7 x
-// 128000 x 4096 53 (5.3). Beyond them a block's wait, reads from LDS, conversions and products
-// follow one another: gated 41 x 9001 x 4008 19.3 us.
+// Up to some 16 rows bound by memory: 7 x 128000 x 4096 52.6 us (5.3 TB/s; the weights, 279 MB,
+// do not stay in a cache), 1 x 4096 x 14336 8.1 (3.9 TB/s with the launch; its 31 MB stay in the
+// last-level cache from one pass to the next, in a graph over 24 such matrices a pass takes 10.0 and
+// with three 9.5). Beyond them a block's wait, reads from LDS, conversions and products
+// follow one another: gated 41 x 9001 x 4008 18.8 us.
 template <typename T, int XR, int NT, int WN, int STAGES, int HALVES, bool DIRECT>
 __global__ __launch_bounds__(XR <= 16 ? 1024 : 512) void f4_matmul_few(F4MatmulArgs a) {
   constexpr int MT = (XR + 15) / 16, COLUMNS = 16 * NT / HALVES;
@@ -491,9 +496,10 @@ __global__ __launch_bounds__(XR <= 16 ? 1024 : 512) void f4_matmul_few(F4MatmulA
 // DIRECT: x goes from memory into LDS, two blocks in turn; it needs 16-byte aligned
 // rows of whole cells. Otherwise it goes through registers.
 //
-// Bound by the matrix instructions, on 54 to 61 % of the cycles at the 1.8 to 2.0 GHz that they
-// leave: 2011 x 4096 x 14336 206 us, gated 3001 x 14336 x 4096 605, both 1.15 to 1.17 PFLOP/s
-// beside the 1.26 of a long run of plain bfloat16 products.
+// The matrix instructions are at work on 54 and 62 % of the cycles, at the 1.9 to 2.0 GHz that they
+// leave; for the rest a block of 128 columns, of which one is on its way ahead, waits for its
+// loads and the other waves, or converts. 2011 x 4096 x 14336 201 us (1.18 PFLOP/s), gated 3001 x
+// 14336 x 4096 593 (1.19), beside the 1.26 of a long run of plain bfloat16 products.
 template <typename T, int MT, int NT, int WN, int WK, int HALVES, bool DIRECT>
 __global__ __launch_bounds__(64 * WN * WK, 2) void f4_matmul_tiled(F4MatmulArgs a) {
   constexpr int TM = 32 * MT, ROWS = TM / WN, LOADS = ROWS / 4;
@@ -732,9 +738,9 @@ int64_t few_groups(const ifq_f4_matmul_desc& d, const Few& f) {
 // Time in us of a kernel of few rows with k shared by `shares` groups of waves: a round of
 // workgroups is its start and end and its turns, each as long as the loads on their way
 // take or as what a CU's workgroups load (KB) and read in LDS. Fitted to 3900 times of
-// 260 sizes (m up to 1300, n from 100 to 128000, k from 64 to 14336) with 11 % between
-// them on the mean; the choice by it takes 1.5 % longer than the best of the kernels,
-// 35 % at worst (6 x 12717 x 10888 gated 54.6 and 42.1).
+// 260 sizes (m up to 1300, n from 100 to 128000, k from 64 to 14336; DIRECT throughout) with
+// 11 % between them on the mean. Among the kernels that plan_of admits the choice by it takes
+// 1.5 % longer than the best, 35 % at worst (6 x 12717 x 10888 gated 54.6 and 42.1).
 float few_time(const Few& f, int lds, int64_t groups, int64_t kb, int shares) {
   const int64_t each = (groups + 255) / 256;       // on the busiest CU
   const int64_t fit = std::max(1, std::min(kLdsBytes / (lds * shares), 16 / (shares * f.wn)));
@@ -761,7 +767,10 @@ Plan plan_of(const ifq_f4_matmul_desc& d) {
   Plan p = {kTiles, 0, 1, ceil_of(d.m, 128) * ceil_of(d.n, 256 / halves)};
   if (p.groups <= 256 && kb >= 2) p.shares = 2;
   float best = d.m <= 32 ? 1e30f : tiles_time(p.groups, kb, p.shares);
-  // as many rows of x as there are, or 48 and 64 of more
+  // As many rows of x as there are, or 48 and 64 of more. Fewer rows a workgroup, with more of
+  // these, are not admitted, though by the estimate they would be faster where k is long or n
+  // small: 64 x 4096 x 14336 17.9 us with 16 rows, 31.1 with 64 (which take 29.1; 96 rows
+  // 26.9), 40 x 1000 x 4096 5.3 and 9.6. They have not been timed there.
   const int xr = d.m <= 4 ? 4 : d.m <= 8 ? 8 : d.m <= 64 ? (int)ceil_of(d.m, 16) * 16 : 0;
   for (int i = 0; i < (int)(sizeof(kFew) / sizeof(kFew[0])); ++i) {
     const Few& f = kFew[i];
@@ -810,7 +819,8 @@ void tiled(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
 
 template <typename T, int HALVES>
 void matmul(F4MatmulArgs& a, const Plan& p, hipStream_t stream) {
-  // whole cells of 16 bytes, and 32-bit offsets within the rows of a tile
+  // whole cells of 16 bytes, and the tiles' 32-bit offsets within their rows (the kernels of few
+  // rows have 64-bit ones, and would not need the last condition)
   const bool direct = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.ld_x % 8 == 0 &&
                       a.k % 8 == 0 && a.ld_x <= (1 << 22);
   if (p.way == kRows)

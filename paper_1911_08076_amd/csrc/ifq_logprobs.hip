@@ -23,7 +23,11 @@ namespace {
 // order, over the complement of the index, so that keys differ and equal values
 // go by the lower index. Of 256 groups of values the k-th largest maximum is a bar that k
 // values at least reach and few others: those are collected, and each one's place
-// is the number of larger ones.
+// is the number of larger ones. A group is one lane's values, or those of two or four lanes
+// beside one another: where all that counts lies in fewer groups than top tokens (rows of
+// few values, all but a range of tokens masked), the bar is the masked ones' value and all
+// others are ranked, each against each. us, and of unmasked rows: 96 x 50001 top 20 with 4096
+// tokens in one range 398 and 17, 64 x 128000 top 64 497 and 20; 1000 x 1000 top 64 41.
 
 struct LogprobArgs {
   const void* x;
@@ -297,8 +301,8 @@ __device__ __forceinline__ int places(int* count, uint64_t some, int lane) {
 
 // Each key of a list at its place among the first k; a list of fewer leaves zeros. LANES lanes
 // count for a key, eight others at a time each (in workgroups of 4 waves 4: 4000 x 4000 top 20
-// 23.9 -> 22.5 us; of 16 one: four spilled registers, 2000 x 32000 55 -> 60). The list has kRankRun
-// keys of 0 behind it.
+// 23.9 -> 22.5 us, but 1000 x 500 top 40 8.8 -> 9.8; of 16 one: four spilled registers, 2000 x 32000
+// 55 -> 60). The list has kRankRun keys of 0 behind it.
 constexpr int kRankRun = 32;
 template <int LANES>
 __device__ __forceinline__ void rank(const uint64_t* list, int count, int k, uint64_t* best) {
@@ -339,7 +343,8 @@ __global__ __launch_bounds__(64 * WAVES, PER == 32 ? 8 : 4) void logprobs_top(Lo
   const int own = blockIdx.x % a.parts, k = a.top;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   // parts of about the same size, so that the last one too has more groups than top tokens: with
-  // fewer all its values are ranked (8 x 200000 top 33 310 us, 17 with this)
+  // fewer all its values are ranked (8 x 200000 top 33 310 us, 17 with this; 500 x 128000 top 20
+  // 67.9 -> 69.7)
   const int from = a.chunks * own / a.parts, to = a.chunks * (own + 1) / a.parts;
   const int base = (from + wave) * (64 * PER);
   float v[PER];

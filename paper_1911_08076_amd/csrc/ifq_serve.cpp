@@ -177,7 +177,7 @@ ifq_status check_f4_matmul(const ifq_f4_matmul_desc* d, bool gated) {
     return fail(IFQ_ERR_INVALID_ARGUMENT, "f4 product: a leading dimension is below its row");
   if (d->ld_w % 16)
     return fail(IFQ_ERR_UNSUPPORTED, "f4 product: ld_w must be a multiple of 16");
-  if (d->ld_w > kMaxProductStride)      // 32-bit offsets within the rows of a tile
+  if (d->ld_w > kMaxProductStride)      // as for the 8-bit product; these kernels' offsets are 64-bit
     return fail(IFQ_ERR_UNSUPPORTED, "f4 product: ld_w may be up to 2^25");
   if (ifq::f4_matmul_groups(*d) > ifq::kMaxGroups)
     return fail(IFQ_ERR_UNSUPPORTED, "f4 product: m x n is too large for one launch");
